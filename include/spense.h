@@ -521,6 +521,86 @@ int spense_obs_prune_24(float* W, int64_t ldw, int64_t N, int64_t K, const float
                         int64_t dense_begin, uint8_t* keep, int64_t ldk, void* ws, size_t ws_bytes,
                         hipStream_t stream);
 
+/*
+ * The norms before and after a block of a decoder layer, fused with the block's gate, the
+ * residual scale and the fp8 quantisation that the next GEMM takes (the steps around the
+ * linear layers of sec. 3.2 and the MLP of sec. 3.3.1, Eq. (4)).  Per token row m:
+ *   t = y * w_post / sqrt(mean_k y^2 + eps)      with post_weight, else t = y
+ *   r = residual_scale * x + gate * t            without y: r = x
+ *   n = r * w / sqrt(mean_k r^2 + eps)           weight NULL: w = 1
+ * all in fp32.  residual receives r in x_type, normed receives n in y_type (both rounded to
+ * nearest even where bf16), q / scales receive n quantised as by spense_quantize_fp8; n is
+ * formed from the fp32 r.  Each output may be NULL, not all of them; q and scales go together.
+ * x, residual: M x K of x_type; y, gate, normed: M x K of y_type; a gate with ldg = 0 is one
+ * row of K shared by all tokens.  post_weight, weight: K of w_type.  Types SPENSE_BF16 or
+ * SPENSE_F32.  residual may be x itself and normed may be y itself (same pointer, leading
+ * dimension and type); other overlaps of an output are not allowed.  A row of zeros gives
+ * codes of zero with scale 1; NaN and infinities go where the formulas take them (NaN codes
+ * are 0xff).
+ * Any K and alignment of whole elements; 16-byte aligned rows (8 for q) with K % 8 == 0 take
+ * the fast path.  One workgroup per row.  Asynchronous, allocates nothing.
+ * SPENSE_ERR_ARG for a NULL x, no output, q without scales, a gate or post_weight without y,
+ * sizes below 0 or above 2^31-1, ld below K, unknown types, a negative or non-finite eps;
+ * SPENSE_ERR_ALIGN for an operand not aligned to its elements.
+ */
+typedef struct spense_block_norm_t {
+  int64_t M, K;
+  const void* x;
+  int64_t ldx;
+  int32_t x_type;
+  int32_t y_type;
+  const void* y; /* the block's output, or NULL: the norm of x alone */
+  int64_t ldy;
+  const void* gate; /* or NULL: 1 */
+  int64_t ldg;
+  const void* post_weight; /* or NULL: no post-norm */
+  const void* weight;
+  int32_t w_type;
+  float residual_scale;
+  float eps;
+  void* residual;
+  int64_t ldr;
+  void* normed;
+  int64_t ldn;
+  uint8_t* q;
+  int64_t ldq;
+  float* scales;
+} spense_block_norm_t;
+
+int spense_block_norm(const spense_block_norm_t* args, hipStream_t stream);
+
+/* The most groups (experts, adapters) of one spense_group_rows call. */
+#define SPENSE_MAX_GROUPS 1024
+
+/*
+ * Group n rows by an index, as the expert and adapter calls below take them: a stable sort.
+ *   order:   n int32, the entries with 0 <= idx < groups sorted by idx, entries of one group
+ *            in ascending order, then all others in ascending order;
+ *   offsets: groups + 1 int32; group g owns positions [offsets[g], offsets[g + 1]) of order,
+ *            offsets[groups] is the number of entries in any group;
+ *   inverse: n int32 or NULL; the position of each entry, -1 where its idx names no group.
+ * idx: n int32 on the device, any values.  Outputs must not overlap idx or each other.  The
+ * result depends on idx only.  One workgroup; asynchronous, allocates nothing.
+ * SPENSE_ERR_ARG for NULL pointers, n below 0 or above 2^31-1, groups outside [1,
+ * SPENSE_MAX_GROUPS].
+ */
+int spense_group_rows(const int32_t* idx, int64_t n, int32_t groups, int32_t* order, int32_t* inverse, int32_t* offsets,
+                      hipStream_t stream);
+
+/*
+ * Sum the rows of each token back: Y[t, :] = sum_j weights[t, j] * D[inverse[t * top + j], :]
+ * over j = 0 .. top - 1 ascending, in fp32, rounded once.  D: n x N of d_type (SPENSE_BF16 or
+ * SPENSE_F32), leading dimension ldd, in the positions of spense_group_rows; inverse: T * top
+ * int32 (entries outside [0, n), e.g. -1, add nothing; a token without any gives zeros);
+ * weights: T * top fp32 or NULL (ones).  Y: T x N, bf16 or fp32 (SPENSE_OUT_F32), leading
+ * dimension ldy; it must not overlap D.  Asynchronous, allocates nothing.  SPENSE_ERR_ARG for
+ * NULL pointers, bad sizes, types or flags, ld below N; SPENSE_ERR_ALIGN for a D or Y not
+ * aligned to its elements.
+ */
+int spense_combine_rows(const void* D, int32_t d_type, int64_t n, int64_t ldd, const int32_t* inverse,
+                        const float* weights, int64_t T, int32_t top, int64_t N, void* Y, int64_t ldy, uint32_t out_flags,
+                        hipStream_t stream);
+
 /* Thread-local description of the last error raised on this thread ("" if none). */
 const char* spense_last_error(void);
 

@@ -12,8 +12,10 @@ tensors.  Paper: SpenseGPT, sec. 3.1.1 (2:4 storage) and sec. 3.2 (Spense format
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -38,6 +40,7 @@ SPENSE_OUT_F32 = 1
 SPENSE_LAYOUT_ROWMAJOR = 0
 SPENSE_LAYOUT_TILED = 1
 SPENSE_NOALLOC_SCRATCH_BYTES = 16 << 20
+SPENSE_MAX_GROUPS = 1024
 
 EXPORTS = ["spense_abi_version", "spense_set_log", "spense_last_error", "spense_layout", "spense_tiled_layout",
            "spense_compress_workspace_size", "spense_compress", "spense_decompress", "spense_tile",
@@ -46,7 +49,7 @@ EXPORTS = ["spense_abi_version", "spense_set_log", "spense_last_error", "spense_
            "spense_gather_rows", "spense_gather_cols", "spense_obs_factor_workspace_size", "spense_obs_factor",
            "spense_obs_prune_workspace_size", "spense_obs_prune_24", "spense_gemm_grouped", "spense_gemm_glu",
            "spense_gemm_glu_pays", "spense_gemm_glu_fp8_workspace_size", "spense_gemm_glu_fp8", "spense_gemm_planned_workspace_size",
-           "spense_gemm_planned", "spense_gemm_noalloc"]
+           "spense_gemm_planned", "spense_gemm_noalloc", "spense_block_norm", "spense_group_rows", "spense_combine_rows"]
 
 
 class SpenseError(RuntimeError):
@@ -81,6 +84,16 @@ class spense_plan_override_t(ctypes.Structure):
                 ("waves_used_dense", ctypes.c_int32), ("waves_used_24", ctypes.c_int32),
                 ("block_order", ctypes.c_int32), ("xcd_order", ctypes.c_int32), ("u8", ctypes.c_int32),
                 ("half_row_blocks", ctypes.c_int32), ("resident_x", ctypes.c_int32)]
+
+
+class spense_block_norm_t(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int64), ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("x_type", ctypes.c_int32), ("y_type", ctypes.c_int32), ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
+                ("gate", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("post_weight", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("w_type", ctypes.c_int32), ("residual_scale", ctypes.c_float),
+                ("eps", ctypes.c_float), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("normed", ctypes.c_void_p), ("ldn", ctypes.c_int64), ("q", ctypes.c_void_p), ("ldq", ctypes.c_int64),
+                ("scales", ctypes.c_void_p)]
 
 
 KERNEL_KSPLIT, KERNEL_ROWS, KERNEL_LARGE_M = 1, 2, 3
@@ -134,6 +147,9 @@ def _load():
         "spense_gemm_glu_fp8": (ctypes.c_int, [p, i64, i64, p, p, p, p, p, p, i64, p, p, ctypes.c_size_t, p]),
         "spense_gemm_planned_workspace_size": (sz, [i64, P(spense_packed_t), P(spense_plan_override_t)]),
         "spense_gemm_noalloc": (ctypes.c_int, [p, i64, i64, P(spense_packed_t), p, p, p, i64, u32, p]),
+        "spense_block_norm": (ctypes.c_int, [P(spense_block_norm_t), p]),
+        "spense_group_rows": (ctypes.c_int, [p, i64, i32, p, p, p, p]),
+        "spense_combine_rows": (ctypes.c_int, [p, i32, i64, i64, p, p, i64, i32, i64, p, i64, u32, p]),
         "spense_gemm_planned": (ctypes.c_int, [p, i64, i64, P(spense_packed_t), p, p, p, i64, u32, p, sz,
                                                P(spense_plan_override_t), p]),
     }
@@ -294,6 +310,18 @@ def spense_obs_prune_workspace_size(N: int) -> int:
 
 def spense_obs_prune_24(W, ldw, N, K, U, ldu, dead, dense_begin, keep, ldk, ws, ws_bytes, stream) -> int:
     return _lib.spense_obs_prune_24(W, ldw, N, K, U, ldu, dead, dense_begin, keep, ldk, ws, ws_bytes, stream)
+
+
+def spense_block_norm(args: spense_block_norm_t, stream) -> int:
+    return _lib.spense_block_norm(ctypes.byref(args), stream)
+
+
+def spense_group_rows(idx, n, groups, order, inverse, offsets, stream) -> int:
+    return _lib.spense_group_rows(idx, n, groups, order, inverse, offsets, stream)
+
+
+def spense_combine_rows(D, d_type, n, ldd, inverse, weights, T, top, N, Y, ldy, out_flags, stream) -> int:
+    return _lib.spense_combine_rows(D, d_type, n, ldd, inverse, weights, T, top, N, Y, ldy, out_flags, stream)
 
 
 # ------------------------------------------------------------------ torch helpers
@@ -800,3 +828,163 @@ def obs_prune_24(W: torch.Tensor, U: torch.Tensor, dense_begin: int, dead: torch
     _check(spense_obs_prune_24(_ptr(W), W.stride(0), N, K, _ptr(U), U.stride(0), _ptr(dead), dense_begin, _ptr(keep),
                                keep.stride(0), wp, wn, _stream(W.device)))
     return keep
+
+
+# ------------------------------------------------------------------ norms around a block
+class BlockNorm(NamedTuple):
+    """What block_norm returns; outputs not asked for are None."""
+
+    residual: torch.Tensor | None
+    normed: torch.Tensor | None
+    codes: torch.Tensor | None
+    scales: torch.Tensor | None
+
+
+_here = contextlib.nullcontext()
+
+
+def _device(dev):
+    """Makes ``dev`` the current device while a call runs whose tensors are on it."""
+    return _here if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+
+def _on_gpu(dev, **tensors):
+    if dev.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, not on {dev}")
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, expected {dev}")
+
+
+def _rows_of(t, name, shape, dtype=None):
+    """A 2-D tensor of this shape with contiguous rows that do not overlap."""
+    _row_major(t, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}'s rows overlap")
+
+
+def _ld(t):
+    """Leading dimension of a 2-D tensor; a single row's stride does not matter."""
+    return max(t.stride(0), t.shape[1])
+
+
+def block_norm(x: torch.Tensor, y: torch.Tensor | None = None, *, post_weight=None, gate=None,
+               residual_scale: float = 1.0, weight=None, eps: float = 1e-6, quantize: bool = True,
+               normed: bool = False, residual_out=None, normed_out=None, codes_out=None, scales_out=None) -> BlockNorm:
+    """The norms before and after a block, fused with its gate, the residual scale and the fp8
+    quantisation (spense_block_norm): with the residual stream x and the block's output y
+    (M x K, bf16 or fp32 each),
+        t = rms_norm(y) * post_weight (y itself without post_weight),
+        r = residual_scale * x + gate * t (x itself without y),  n = rms_norm(r) * weight.
+    Returns (residual r in x's type, None without y; normed n in y's type (x's without y) where
+    ``normed``; codes uint8 M x K and scales fp32 M of n where ``quantize``).  gate: K entries shared by
+    all tokens, or M x K, of y's type; post_weight, weight: K entries of one type, bf16 or fp32.
+    residual_out may be x and normed_out may be y."""
+    _row_major(x, "x")
+    M, K = x.shape
+    dev = x.device
+    xt = _act_type(x)
+    if y is None:
+        if gate is not None or post_weight is not None:
+            raise ValueError("gate and post_weight need a block output y")
+        yt, ydtype = xt, x.dtype
+    else:
+        _rows_of(y, "y", (M, K))
+        yt, ydtype = _act_type(y), y.dtype
+    ldg = 0
+    if gate is not None:
+        if gate.dtype != ydtype:
+            raise ValueError(f"gate is {gate.dtype}, expected {ydtype}")
+        if gate.dim() == 1:
+            if gate.shape[0] != K or not gate.is_contiguous():
+                raise ValueError(f"gate must be a contiguous vector of length {K} or of shape {(M, K)}")
+        else:
+            _rows_of(gate, "gate", (M, K))
+            ldg = _ld(gate)
+    wt = None
+    for w, name in ((post_weight, "post_weight"), (weight, "weight")):
+        if w is None:
+            continue
+        if w.dim() != 1 or w.shape[0] != K or not w.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous vector of length {K}")
+        if wt is not None and _act_type(w) != wt:
+            raise ValueError("post_weight and weight must have one type")
+        wt = _act_type(w)
+    normed = normed or normed_out is not None
+    quantize = quantize or codes_out is not None or scales_out is not None
+    if y is None and residual_out is not None:
+        raise ValueError("without y there is no new residual")
+    _on_gpu(dev, y=y, gate=gate, post_weight=post_weight, weight=weight, residual_out=residual_out,
+            normed_out=normed_out, codes_out=codes_out, scales_out=scales_out)
+    r = n = q = s = None
+    if y is not None:
+        r = torch.empty((M, K), dtype=x.dtype, device=dev) if residual_out is None else residual_out
+        _rows_of(r, "residual_out", (M, K), x.dtype)
+    if normed:
+        n = torch.empty((M, K), dtype=ydtype, device=dev) if normed_out is None else normed_out
+        _rows_of(n, "normed_out", (M, K), ydtype)
+    if quantize:
+        q = torch.empty((M, K), dtype=torch.uint8, device=dev) if codes_out is None else codes_out
+        s = torch.empty(M, dtype=torch.float32, device=dev) if scales_out is None else scales_out
+        _rows_of(q, "codes_out", (M, K), torch.uint8)
+        _check_scale(s, M, dev, "scales_out")
+    if r is None and n is None and q is None:
+        raise ValueError("no output is asked for")
+    a = spense_block_norm_t(M, K, _ptr(x), _ld(x), xt, yt, _ptr(y), 0 if y is None else _ld(y), _ptr(gate), ldg,
+                            _ptr(post_weight), _ptr(weight), wt or SPENSE_F32, residual_scale, eps, _ptr(r),
+                            0 if r is None else _ld(r), _ptr(n), 0 if n is None else _ld(n), _ptr(q),
+                            0 if q is None else _ld(q), _ptr(s))
+    with _device(dev):
+        _check(spense_block_norm(a, _stream(dev)))
+    return BlockNorm(r, n, q, s)
+
+
+# ------------------------------------------------------------------ rows grouped by expert or adapter
+class RowGroups:
+    """n rows grouped by an index (spense_group_rows), for any number of calls on the same rows:
+    ``order`` (n int32, the rows of group 0, 1, ... and then those of no group), ``offsets``
+    (groups + 1 int32, group g owns positions [offsets[g], offsets[g + 1])) and ``inverse`` (n int32,
+    each row's position, -1 where it is in no group), all on the device."""
+
+    def __init__(self, n, groups, order, inverse, offsets):
+        self.n, self.groups = n, groups
+        self.order, self.inverse, self.offsets = order, inverse, offsets
+
+
+def group_rows(idx: torch.Tensor, groups: int) -> RowGroups:
+    """Group rows by idx (int32, 1-D, any values: those outside [0, groups) are in no group)."""
+    if idx.dtype != torch.int32 or idx.dim() != 1 or not idx.is_contiguous():
+        raise ValueError("idx must be a contiguous int32 vector")
+    dev = idx.device
+    _on_gpu(dev)
+    n = idx.numel()
+    buf = torch.empty(2 * n + max(groups, 0) + 1, dtype=torch.int32, device=dev)
+    order, inverse, offsets = buf[:n], buf[n:2 * n], buf[2 * n:]
+    with _device(dev):
+        _check(spense_group_rows(_ptr(idx), n, groups, _ptr(order), _ptr(inverse), _ptr(offsets), _stream(dev)))
+    return RowGroups(n, groups, order, inverse, offsets)
+
+
+def combine_rows(D: torch.Tensor, groups: RowGroups, weights: torch.Tensor | None = None, top: int = 1, out=None,
+                 out_f32: bool = False) -> torch.Tensor:
+    """Y[t] = sum_j weights[t, j] * D[position of row t * top + j], fp32 sums in order of j
+    (spense_combine_rows).  D: n x N in the positions of ``groups`` (bf16 or fp32); weights: T x top
+    fp32 with T = n / top.  Rows in no group add nothing."""
+    _row_major(D, "D")
+    n, N = D.shape
+    if top < 1 or groups.n != n or n % top:
+        raise ValueError(f"D has {n} rows, the groups {groups.n}; both must be T * top with top = {top}")
+    T = n // top
+    dev = D.device
+    _on_gpu(dev, groups=groups.order, weights=weights)
+    if weights is not None and (weights.dtype != torch.float32 or weights.numel() != n or not weights.is_contiguous()):
+        raise ValueError(f"weights must be a contiguous fp32 tensor of {n} entries")
+    out = _out(out, T, N, out_f32, dev)
+    with _device(dev):
+        _check(spense_combine_rows(_ptr(D), _act_type(D), n, _ld(D), _ptr(groups.inverse), _ptr(weights), T, top, N,
+                                   _ptr(out), _ld(out), SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, _stream(dev)))
+    return out

@@ -1211,6 +1211,15 @@ int api_fail(int code, const char* fmt, ...) {
   va_end(ap);
   return code;
 }
+
+int api_ok() { return ok(); }
+
+int api_check_device() { return check_device(); }
+
+int api_check_packed(const spense_packed_t* P) {
+  spense_layout_t L;
+  return check_packed(P, &L);
+}
 }  // namespace spense
 
 extern "C" {

@@ -1,0 +1,231 @@
+// Rows grouped by an index (expert or adapter), and the rows of a token's experts summed back.
+//
+// Grouping is a stable counting sort in one workgroup: each wave counts the keys of its
+// contiguous part of the index array in its own LDS row, the rows' prefix over waves and the
+// counts' prefix over groups give every (wave, group) its first position, and a second walk
+// over the same entries places them.  Inside a step of 64 entries a lane finds the lanes with
+// its key by ballots over the key's bits; its rank is the number of lower ones.  No atomics:
+// the order is the index order, whatever the timing.
+//
+// Latency-bound: n = 64 to 512 takes one step a wave and pass; every further 1024 entries
+// (512 above 511 groups) one more.
+#include <hip/hip_runtime.h>
+
+#include "spense.h"
+#include "spense_internal.h"
+
+namespace spense {
+namespace {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+// LDS traffic of other lanes of this wave happens between the statements around it.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// NW waves, GMAX keys (the groups and one for entries outside them).
+template <int NW, int GMAX>
+__global__ __launch_bounds__(64 * NW) void group_rows_kernel(const int32_t* __restrict__ idx, int64_t n, int groups, int bits,
+                                                             int32_t* __restrict__ order, int32_t* __restrict__ inverse,
+                                                             int32_t* __restrict__ offsets) {
+  __shared__ int cnt[NW][GMAX];
+  __shared__ int base[GMAX];
+  __shared__ int wsum[NW];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t part = ((n + NW - 1) / NW + 63) / 64 * 64;  // entries of a wave
+  const int64_t i0 = wave * part, i1 = min(n, i0 + part);
+  for (int g = threadIdx.x; g < NW * GMAX; g += 64 * NW) (&cnt[0][0])[g] = 0;
+  __syncthreads();
+  // lanes of this wave with this lane's key (its own included); all lanes take part
+  auto peers = [&](int key) {
+    uint64_t m = ~0ull;
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t set = __ballot((key >> b) & 1);
+      m &= (key >> b) & 1 ? set : ~set;
+    }
+    return m;
+  };
+  auto key_of = [&](int64_t i) {  // entries past the part get the key `groups` and are masked
+    const int v = i < i1 ? idx[i] : -1;
+    return v >= 0 && v < groups ? v : groups;
+  };
+  const uint64_t below = (1ull << lane) - 1;
+  int key = key_of(i0 + lane);
+  for (int64_t i = i0; i < i1; i += 64) {
+    const int next = key_of(i + 64 + lane);
+    const uint64_t m = peers(key) & __ballot(i + lane < i1);
+    if (i + lane < i1 && !(m & below)) cnt[wave][key] += __popcll(m);
+    wave_fence();
+    key = next;
+  }
+  __syncthreads();
+  // prefix over the waves of each key, then over the keys
+  for (int g0 = 0; g0 <= groups; g0 += 64 * NW) {
+    const int g = g0 + threadIdx.x;
+    int tot = 0;
+    if (g <= groups) {
+      for (int w = 0; w < NW; ++w) {
+        const int c = cnt[w][g];
+        cnt[w][g] = tot;
+        tot += c;
+      }
+    }
+    int inc = tot;  // inclusive prefix over the workgroup
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(inc, o, 64);
+      if (lane >= o) inc += u;
+    }
+    if (lane == 63) wsum[wave] = inc;
+    __syncthreads();
+    int before = g0 ? base[g0 - 1] : 0;  // base[g]: the entries with keys up to g
+    for (int w = 0; w < wave; ++w) before += wsum[w];
+    if (g <= groups) base[g] = before + inc;
+    __syncthreads();
+  }
+  for (int g = threadIdx.x; g <= groups; g += 64 * NW) offsets[g] = g ? base[g - 1] : 0;
+  key = key_of(i0 + lane);
+  for (int64_t i = i0; i < i1; i += 64) {
+    const int next = key_of(i + 64 + lane);
+    const bool in = i + lane < i1;
+    const uint64_t m = peers(key) & __ballot(in);
+    const int first = cnt[wave][key];
+    wave_fence();
+    if (in && !(m & below)) cnt[wave][key] = first + __popcll(m);
+    wave_fence();
+    if (in) {
+      const int p = (key ? base[key - 1] : 0) + first + __popcll(m & below);
+      order[p] = (int32_t)(i + lane);
+      if (inverse) inverse[i + lane] = key < groups ? p : -1;
+    }
+    key = next;
+  }
+}
+
+// Y[t] = sum_j w[t, j] * D[inverse[t * top + j]] in fp32, j ascending; entries without a row
+// (-1, or outside [0, n)) add nothing.  A workgroup takes 256 * E columns of a token.
+template <bool DBF, bool YBF, int E>
+__global__ __launch_bounds__(256) void combine_rows_kernel(const uint8_t* __restrict__ D, int64_t ldd_b, int64_t n,
+                                                           const int32_t* __restrict__ inverse, const float* __restrict__ w,
+                                                           int top, int64_t N, uint8_t* __restrict__ Y, int64_t ldy_b,
+                                                           int blocks) {
+  const int64_t t = blockIdx.x / blocks;
+  const int64_t c = ((int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x) * E;
+  if (c >= N) return;
+  float acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+  for (int j = 0; j < top; ++j) {
+    const int p = inverse[t * top + j];
+    if (p < 0 || p >= n) continue;
+    const float wj = w ? w[t * top + j] : 1.0f;
+    const uint8_t* row = D + (int64_t)p * ldd_b;
+    float v[E];
+    if constexpr (E == 1) {
+      v[0] = DBF ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[c] << 16)
+                 : reinterpret_cast<const float*>(row)[c];
+    } else if constexpr (DBF) {
+      typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+      const u2 d = *reinterpret_cast<const u2*>(row + 2 * c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(e & 1 ? d[e / 2] & 0xffff0000u : d[e / 2] << 16);
+    } else {
+      const v4f d = *reinterpret_cast<const v4f*>(row + 4 * c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = d[e];
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(wj, v[e], acc[e]);
+  }
+  uint8_t* yr = Y + t * ldy_b;
+  auto bf = [](float f) {
+    __bf16 h = (__bf16)f;
+    return (uint32_t)__builtin_bit_cast(uint16_t, h);
+  };
+  if constexpr (E == 1) {
+    if constexpr (YBF)
+      reinterpret_cast<uint16_t*>(yr)[c] = (uint16_t)bf(acc[0]);
+    else
+      reinterpret_cast<float*>(yr)[c] = acc[0];
+  } else if constexpr (YBF) {
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    *reinterpret_cast<u2*>(yr + 2 * c) = (u2){bf(acc[0]) | (bf(acc[1]) << 16), bf(acc[2]) | (bf(acc[3]) << 16)};
+  } else {
+    *reinterpret_cast<v4f*>(yr + 4 * c) = (v4f){acc[0], acc[1], acc[2], acc[3]};
+  }
+}
+
+template <bool DBF, bool YBF>
+hipError_t launch_combine(const uint8_t* D, int64_t ldd_b, int64_t n, const int32_t* inverse, const float* w, int64_t T,
+                          int top, int64_t N, uint8_t* Y, int64_t ldy_b, bool vec, hipStream_t st) {
+  const int64_t per = vec ? 1024 : 256, blocks = (N + per - 1) / per;
+  const dim3 grid((unsigned)(T * blocks));
+  if (vec)
+    hipLaunchKernelGGL((combine_rows_kernel<DBF, YBF, 4>), grid, dim3(256), 0, st, D, ldd_b, n, inverse, w, top, N, Y, ldy_b,
+                       (int)blocks);
+  else
+    hipLaunchKernelGGL((combine_rows_kernel<DBF, YBF, 1>), grid, dim3(256), 0, st, D, ldd_b, n, inverse, w, top, N, Y, ldy_b,
+                       (int)blocks);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace spense
+
+using spense::api_fail;
+
+extern "C" {
+
+int spense_group_rows(const int32_t* idx, int64_t n, int32_t groups, int32_t* order, int32_t* inverse, int32_t* offsets,
+                      hipStream_t stream) {
+  if (n < 0 || n > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "bad n=%lld", (long long)n);
+  if (groups < 1 || groups > SPENSE_MAX_GROUPS)
+    return api_fail(SPENSE_ERR_ARG, "groups=%d outside [1, %d]", groups, SPENSE_MAX_GROUPS);
+  if (!offsets || (n > 0 && (!idx || !order))) return api_fail(SPENSE_ERR_ARG, "NULL pointer");
+  int rc = spense::api_check_device();
+  if (rc) return rc;
+  int bits = 1;
+  while ((groups >> bits) != 0) ++bits;  // keys 0 .. groups
+  if (groups < 512)
+    hipLaunchKernelGGL((spense::group_rows_kernel<16, 512>), dim3(1), dim3(1024), 0, stream, idx, n, groups, bits, order,
+                       inverse, offsets);
+  else
+    hipLaunchKernelGGL((spense::group_rows_kernel<8, SPENSE_MAX_GROUPS + 1>), dim3(1), dim3(512), 0, stream, idx, n, groups,
+                       bits, order, inverse, offsets);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return api_fail(SPENSE_ERR_HIP, "group rows launch failed: %s", hipGetErrorString(e));
+  return spense::api_ok();
+}
+
+int spense_combine_rows(const void* D, int32_t d_type, int64_t n, int64_t ldd, const int32_t* inverse,
+                        const float* weights, int64_t T, int32_t top, int64_t N, void* Y, int64_t ldy, uint32_t out_flags,
+                        hipStream_t stream) {
+  if (d_type != SPENSE_BF16 && d_type != SPENSE_F32) return api_fail(SPENSE_ERR_ARG, "d_type %d is not bf16 or f32", d_type);
+  if (n < 0 || T < 0 || N < 0 || top < 1 || n > INT32_MAX || T > INT32_MAX || N > INT32_MAX || T * top > INT32_MAX)
+    return api_fail(SPENSE_ERR_ARG, "bad n=%lld T=%lld top=%d N=%lld", (long long)n, (long long)T, top, (long long)N);
+  if (out_flags & ~1u) return api_fail(SPENSE_ERR_ARG, "unknown out_flags 0x%x", out_flags);
+  if (T == 0 || N == 0) return spense::api_ok();
+  if ((n > 0 && !D) || !inverse || !Y) return api_fail(SPENSE_ERR_ARG, "NULL pointer");
+  if ((n > 0 && ldd < N) || ldy < N) return api_fail(SPENSE_ERR_ARG, "leading dimension below N");
+  const int64_t ds = d_type == SPENSE_BF16 ? 2 : 4, ys = (out_flags & SPENSE_OUT_F32) ? 4 : 2;
+  const uintptr_t dp = reinterpret_cast<uintptr_t>(D), yp = reinterpret_cast<uintptr_t>(Y);
+  if (dp % ds || yp % ys) return api_fail(SPENSE_ERR_ALIGN, "D or Y misaligned");
+  if (T * ((N + 255) / 256) > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "T x N too large for the grid");
+  int rc = spense::api_check_device();
+  if (rc) return rc;
+  // four columns a thread where D's and Y's quads are aligned
+  const bool vec = N % 4 == 0 && dp % (4 * ds) == 0 && ldd % 4 == 0 && yp % (4 * ys) == 0 && ldy % 4 == 0;
+  const uint8_t* d8 = static_cast<const uint8_t*>(D);
+  uint8_t* y8 = static_cast<uint8_t*>(Y);
+  const bool db = d_type == SPENSE_BF16, yb = ys == 2;
+  auto go = [&](auto f) { return f(d8, ldd * ds, n, inverse, weights, T, top, N, y8, ldy * ys, vec, stream); };
+  const hipError_t e = db ? (yb ? go(spense::launch_combine<true, true>) : go(spense::launch_combine<true, false>))
+                          : (yb ? go(spense::launch_combine<false, true>) : go(spense::launch_combine<false, false>));
+  if (e != hipSuccess) return api_fail(SPENSE_ERR_HIP, "combine launch failed: %s", hipGetErrorString(e));
+  return spense::api_ok();
+}
+
+}  // extern "C"

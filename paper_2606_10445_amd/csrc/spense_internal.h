@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "spense.h"
+
 namespace spense {
 
 enum : int32_t { kFP8 = 1, kBF16 = 2 };
@@ -121,6 +123,11 @@ hipError_t launch_gemm(int dtype, const LaunchShape& ls, const GemmArgs& a, hipS
 
 // Record an error message for spense_last_error (printf format) and return code.
 int api_fail(int code, const char* fmt, ...);
+// Success: clear this thread's message.  The device check and the check of a packed weight's
+// descriptor that every call makes.
+int api_ok();
+int api_check_device();
+int api_check_packed(const spense_packed_t* P);
 
 // Y for the rows of K-sliced regions: the sum of their fp32 partials in slice order, then
 // the epilogue (after launch_gemm, on the same stream).
