@@ -601,6 +601,50 @@ int spense_combine_rows(const void* D, int32_t d_type, int64_t n, int64_t ldd, c
                         const float* weights, int64_t T, int32_t top, int64_t N, void* Y, int64_t ldy, uint32_t out_flags,
                         hipStream_t stream);
 
+/*
+ * A pool of low-rank adapters of one projection: A count x R x K and B count x N x R bf16,
+ * contiguous and 16-byte aligned device buffers of the caller; scale: count fp32 or NULL
+ * (ones).  R is a multiple of 8 from 8 to 128 (adapters of smaller rank: rows of zeros in A
+ * or columns of zeros in B), K a multiple of 32, count in [1, SPENSE_MAX_GROUPS].
+ */
+typedef struct spense_adapters_t {
+  int32_t count, R;
+  int64_t K, N;
+  const void* A;
+  const void* B;
+  const float* scale;
+} spense_adapters_t;
+
+/* Device workspace (bytes) of spense_add_adapters for M tokens: fp32 partial sums of A x, up
+ * to 16 x M x R of them (0 for a pool or an M that the call refuses). */
+size_t spense_adapters_workspace_size(int64_t M, const spense_adapters_t* pool);
+
+/*
+ * The adapters of many requests beside a projection they share (the linear layer of sec. 3.2
+ * with the low-rank update of each token's request added to it):
+ *   Y[m, :] = base[m, :] + scale[a] * B_a (A_a x_m),   a the adapter of token m,
+ *   Y[m, :] = base[m, :]                               for a token without one.
+ * X: M x K activations of x_type, SPENSE_FP8_E4M3FN codes (with x_scale, M fp32 or NULL, as in
+ * spense_gemm) or SPENSE_BF16, leading dimension ldx; order (M) and offsets (count + 1) as
+ * written by spense_group_rows for the tokens' adapter indices and pool->count groups: one
+ * grouping serves every projection of a step.  base: M x N of base_type (SPENSE_BF16 or
+ * SPENSE_F32), the projection's output; Y: M x N, bf16 or fp32 (SPENSE_OUT_F32).  Y may be
+ * base itself (same pointer, type and leading dimension: rows without an adapter are then not
+ * touched); otherwise they must not overlap.
+ * A x is summed in fp32, B V in fp32 with V to 16 bits or more of its fp32 value, added to base and
+ * rounded once.  The order of the sums depends on the sizes only.  Two launches, asynchronous;
+ * ws is scratch between them, caller-owned; calls that overlap on one workspace race.
+ * order entries outside [0, M) are skipped, offsets are clamped to [0, M].
+ * SPENSE_ERR_ARG for NULL pointers, bad sizes or types, an R or count outside the limits above,
+ * ld below the row length, a Y = base of another type or pitch, X or one adapter of 2 GiB or
+ * more; SPENSE_ERR_ALIGN for X, A, B or ws not 16-byte aligned (ldx a multiple of 16 bytes),
+ * K % 32, base or Y not aligned to its elements; SPENSE_ERR_WS for a missing or small workspace.
+ */
+int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, const float* x_scale, const int32_t* order,
+                        const int32_t* offsets, const spense_adapters_t* pool, const void* base, int32_t base_type,
+                        int64_t ldb, void* Y, int64_t ldy, uint32_t out_flags, void* ws, size_t ws_bytes,
+                        hipStream_t stream);
+
 /* Thread-local description of the last error raised on this thread ("" if none). */
 const char* spense_last_error(void);
 

@@ -49,7 +49,8 @@ EXPORTS = ["spense_abi_version", "spense_set_log", "spense_last_error", "spense_
            "spense_gather_rows", "spense_gather_cols", "spense_obs_factor_workspace_size", "spense_obs_factor",
            "spense_obs_prune_workspace_size", "spense_obs_prune_24", "spense_gemm_grouped", "spense_gemm_glu",
            "spense_gemm_glu_pays", "spense_gemm_glu_fp8_workspace_size", "spense_gemm_glu_fp8", "spense_gemm_planned_workspace_size",
-           "spense_gemm_planned", "spense_gemm_noalloc", "spense_block_norm", "spense_group_rows", "spense_combine_rows"]
+           "spense_gemm_planned", "spense_gemm_noalloc", "spense_block_norm", "spense_group_rows", "spense_combine_rows",
+           "spense_adapters_workspace_size", "spense_add_adapters"]
 
 
 class SpenseError(RuntimeError):
@@ -94,6 +95,11 @@ class spense_block_norm_t(ctypes.Structure):
                 ("eps", ctypes.c_float), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
                 ("normed", ctypes.c_void_p), ("ldn", ctypes.c_int64), ("q", ctypes.c_void_p), ("ldq", ctypes.c_int64),
                 ("scales", ctypes.c_void_p)]
+
+
+class spense_adapters_t(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int32), ("R", ctypes.c_int32), ("K", ctypes.c_int64), ("N", ctypes.c_int64),
+                ("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 KERNEL_KSPLIT, KERNEL_ROWS, KERNEL_LARGE_M = 1, 2, 3
@@ -150,6 +156,9 @@ def _load():
         "spense_block_norm": (ctypes.c_int, [P(spense_block_norm_t), p]),
         "spense_group_rows": (ctypes.c_int, [p, i64, i32, p, p, p, p]),
         "spense_combine_rows": (ctypes.c_int, [p, i32, i64, i64, p, p, i64, i32, i64, p, i64, u32, p]),
+        "spense_adapters_workspace_size": (sz, [i64, P(spense_adapters_t)]),
+        "spense_add_adapters": (ctypes.c_int, [p, i32, i64, i64, p, p, p, P(spense_adapters_t), p, i32, i64, p, i64,
+                                               u32, p, sz, p]),
         "spense_gemm_planned": (ctypes.c_int, [p, i64, i64, P(spense_packed_t), p, p, p, i64, u32, p, sz,
                                                P(spense_plan_override_t), p]),
     }
@@ -322,6 +331,16 @@ def spense_group_rows(idx, n, groups, order, inverse, offsets, stream) -> int:
 
 def spense_combine_rows(D, d_type, n, ldd, inverse, weights, T, top, N, Y, ldy, out_flags, stream) -> int:
     return _lib.spense_combine_rows(D, d_type, n, ldd, inverse, weights, T, top, N, Y, ldy, out_flags, stream)
+
+
+def spense_adapters_workspace_size(M: int, pool: spense_adapters_t) -> int:
+    return _lib.spense_adapters_workspace_size(M, ctypes.byref(pool))
+
+
+def spense_add_adapters(X, x_type, M, ldx, x_scale, order, offsets, pool: spense_adapters_t, base, base_type, ldb, Y,
+                        ldy, out_flags, ws, ws_bytes, stream) -> int:
+    return _lib.spense_add_adapters(X, x_type, M, ldx, x_scale, order, offsets, ctypes.byref(pool), base, base_type,
+                                    ldb, Y, ldy, out_flags, ws, ws_bytes, stream)
 
 
 # ------------------------------------------------------------------ torch helpers
@@ -988,3 +1007,71 @@ def combine_rows(D: torch.Tensor, groups: RowGroups, weights: torch.Tensor | Non
         _check(spense_combine_rows(_ptr(D), _act_type(D), n, _ld(D), _ptr(groups.inverse), _ptr(weights), T, top, N,
                                    _ptr(out), _ld(out), SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, _stream(dev)))
     return out
+
+
+# ------------------------------------------------------------------ low-rank adapters beside a projection
+class AdapterPool:
+    """The low-rank adapters of one projection: A (count x R x K) and B (count x N x R), bf16 and
+    contiguous, and their scales (count fp32, or None for ones).  R is a multiple of 8 up to 128;
+    adapters of smaller rank have zeros in the rest."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None):
+        if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+            raise ValueError("A must be count x R x K and B count x N x R")
+        if A.dtype != torch.bfloat16 or B.dtype != torch.bfloat16:
+            raise ValueError("A and B must be bfloat16")
+        if not A.is_contiguous() or not B.is_contiguous():
+            raise ValueError("A and B must be contiguous")
+        self.count, self.R, self.K = A.shape
+        self.N = B.shape[1]
+        self.device = A.device
+        _on_gpu(self.device, B=B)
+        _check_scale(scale, self.count, self.device, "scale")
+        self.A, self.B, self.scale = A, B, scale
+        self.desc = spense_adapters_t(self.count, self.R, self.K, self.N, _ptr(A), _ptr(B), _ptr(scale))
+
+
+def add_adapters(base: torch.Tensor, X: torch.Tensor, pool: AdapterPool, groups: RowGroups, x_scale=None, out=None,
+                 out_f32: bool = False, workspace: Workspace | None = None) -> torch.Tensor:
+    """Y[m] = base[m] + scale[a] * B_a (A_a x_m) for the adapter a of each token (spense_add_adapters).
+    base: M x N, bf16 or fp32, the projection's output; X: M x K, bf16 or fp8 codes with x_scale;
+    groups: group_rows of the tokens' adapter indices over pool.count groups (tokens of no group get
+    base).  out may be base."""
+    _row_major(X, "X")
+    _row_major(base, "base")
+    M = X.shape[0]
+    dev = X.device
+    xt = SPENSE_BF16 if X.dtype == torch.bfloat16 else _act_code(X)
+    if xt is None or X.dtype in (torch.int16, torch.uint16):
+        raise ValueError(f"X is {X.dtype}; adapters take fp8 codes (uint8) or bfloat16")
+    if X.shape[1] != pool.K:
+        raise ValueError(f"X.shape[1] = {X.shape[1]} != K = {pool.K}")
+    _rows_of(base, "base", (M, pool.N))
+    bt = _act_type(base)
+    if groups.n != M or groups.groups != pool.count:
+        raise ValueError(f"groups are of {groups.n} rows over {groups.groups}, expected {M} over {pool.count}")
+    _on_gpu(dev, base=base, pool=pool.A, groups=groups.order)
+    _check_scale(x_scale, M, dev, "x_scale")
+    out = _out(out, M, pool.N, out_f32, dev)
+    ws = workspace or _CallScratch(dev)
+    with _device(dev):
+        wp, wn = ws.get(spense_adapters_workspace_size(M, pool.desc))
+        _check(spense_add_adapters(_ptr(X), xt, M, _ld(X), _ptr(x_scale), _ptr(groups.order), _ptr(groups.offsets),
+                                   pool.desc, _ptr(base), bt, _ld(base), _ptr(out), _ld(out),
+                                   SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, wp, wn, _stream(dev)))
+    return out
+
+
+def gemm_adapters(X: torch.Tensor, pw: PackedWeight, pool: AdapterPool, groups: RowGroups, w_scale=None, x_scale=None,
+                  A_x: torch.Tensor | None = None, out=None, out_f32: bool = False,
+                  workspace: Workspace | None = None) -> torch.Tensor:
+    """A projection with each token's adapter: X W^T (gemm, in fp32) + scale[a] * B_a (A_a x), rounded
+    once.  A_x: the activations the adapters see, where they are not X's codes (bf16, e.g. the
+    unquantised output of block_norm)."""
+    if pw.N != pool.N:
+        raise ValueError(f"the weight has {pw.N} rows, the adapters {pool.N}")
+    base = gemm(X, pw, w_scale, x_scale, out_f32=True, workspace=workspace)
+    if A_x is not None:
+        X, x_scale = A_x, None
+    return add_adapters(base, X, pool, groups, x_scale, out=base if out_f32 and out is None else out, out_f32=out_f32,
+                        workspace=workspace)

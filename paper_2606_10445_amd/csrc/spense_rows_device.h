@@ -1,0 +1,74 @@
+// Device helper of the kernels that work on rows grouped by an index (spense_group_rows).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace spense {
+namespace {
+
+struct RowTile {
+  int group;   // count: the rows of no group
+  int p0, p1;  // positions [p0, p1), at most T of them
+};
+
+// Tile g of the tiles of T positions that the groups are cut into, group by group (with
+// `rest`, then those of the positions in no group); false past the last one.  A tile never
+// spans two groups.  The whole wave calls it with the same arguments; each lane counts a
+// contiguous share of the groups, so the search costs one load latency and a prefix over the
+// lanes.  Offsets are clamped to [0, n] and to ascend, so a tile lies in [0, n) whatever they hold.
+__device__ __forceinline__ bool find_tile(const int32_t* __restrict__ offsets, int count, int n, bool rest, int T, int g,
+                                          RowTile& out) {
+  const int lane = threadIdx.x & 63;
+  const int groups = rest ? count + 1 : count;
+  const int per = (groups + 63) >> 6;
+  auto segment = [&](int e, int& a, int& b) {
+    a = min(max(offsets[e], 0), n);
+    b = e < count ? max(min(max(offsets[e + 1], 0), n), a) : n;
+  };
+  int sum = 0;
+  for (int i = 0; i < per; ++i) {
+    const int e = lane * per + i;
+    if (e < groups) {
+      int a, b;
+      segment(e, a, b);
+      sum += (b - a + T - 1) / T;
+    }
+  }
+  int inc = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += u;
+  }
+  const uint64_t mine = __ballot(g >= inc - sum && g < inc);
+  if (!mine) return false;
+  int at = g - (inc - sum), e = 0, p0 = 0, p1 = 0;
+  bool found = false;
+  for (int i = 0; i < per; ++i) {
+    const int f = lane * per + i;
+    if (f < groups && !found) {
+      int a, b;
+      segment(f, a, b);
+      const int tiles = (b - a + T - 1) / T;
+      if (at >= 0 && at < tiles) {
+        e = f, p0 = a + at * T, p1 = min(b, p0 + T);
+        found = true;
+      }
+      at -= tiles;
+    }
+  }
+  const int src = __builtin_ctzll(mine);
+  out.group = __builtin_amdgcn_readlane(e, src);
+  out.p0 = __builtin_amdgcn_readlane(p0, src);
+  out.p1 = __builtin_amdgcn_readlane(p1, src);
+  return true;
+}
+
+// Most tiles that find_tile can give (host).
+inline int64_t most_tiles(int64_t n, int64_t count, bool rest, int64_t T) {
+  const int64_t groups = count + (rest ? 1 : 0);
+  return n / T + (groups < n ? groups : n);
+}
+
+}  // namespace
+}  // namespace spense

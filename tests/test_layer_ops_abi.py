@@ -52,3 +52,44 @@ def test_combine_rows_refuses(S):
                      (dict(Y=A + 1), -2), (dict(T=1 << 24, N=1 << 20, ldd=1 << 20, ldy=1 << 20), -1)):
         assert S.spense_combine_rows(**{**good, **kw}) == code, kw
     assert S.spense_combine_rows(**{**good, "T": 0}) == 0 and S.spense_combine_rows(**{**good, "N": 0, "Y": None}) == 0
+
+
+def pool(S, **kw):
+    return S.spense_adapters_t(**{**dict(count=4, R=16, K=64, N=48, A=A, B=A, scale=None), **kw})
+
+
+def test_add_adapters_refuses(S):
+    good = dict(X=A, x_type=2, M=8, ldx=64, x_scale=None, order=A, offsets=A, base=A, base_type=3, ldb=48, Y=2 * A, ldy=48,
+                out_flags=0, ws=A, ws_bytes=1 << 20, stream=None)
+
+    def call(pool_kw={}, **kw):
+        return S.spense_add_adapters(pool=pool(S, **pool_kw), **{**good, **kw})
+
+    for kw, code in ((dict(X=None), -1), (dict(order=None), -1), (dict(offsets=None), -1), (dict(base=None), -1),
+                     (dict(Y=None), -1), (dict(x_type=3), -1), (dict(base_type=1), -1), (dict(out_flags=4), -1),
+                     (dict(M=-1), -1), (dict(M=1 << 31), -1), (dict(ldx=63), -1), (dict(ldb=47), -1), (dict(ldy=47), -1),
+                     (dict(X=A + 2), -2), (dict(ldx=68), -2), (dict(base=A + 2), -2), (dict(Y=A + 1), -2),
+                     (dict(Y=A), -1),  # base in the place of Y, of another type
+                     (dict(Y=A, out_flags=1, ldy=64), -1), (dict(ws=None), -4), (dict(ws_bytes=0), -4),
+                     (dict(ws=A + 8), -2), (dict(M=1 << 25), -1)):
+        assert call(**kw) == code, kw
+    for kw, code in ((dict(count=0), -1), (dict(count=1025), -1), (dict(R=0), -1), (dict(R=12), -1), (dict(R=136), -1),
+                     (dict(K=0), -1), (dict(N=0), -1), (dict(K=48), -2), (dict(A=None), -1), (dict(B=None), -1),
+                     (dict(A=A + 8), -2), (dict(K=1 << 27), -1)):
+        assert call(kw, ldx=max(64, kw.get("K", 64))) == code, kw
+        if "A" not in kw and "B" not in kw and kw.get("K") != 1 << 27:
+            assert S.spense_adapters_workspace_size(8, pool(S, **kw)) == 0
+    assert S._lib.spense_add_adapters(A, 2, 8, 64, None, A, A, None, A, 3, 48, A, 48, 0, A, 1 << 20, None) == -1
+    assert call(M=0) == 0 and S.spense_adapters_workspace_size(0, pool(S)) == 0
+    need = S.spense_adapters_workspace_size(8, pool(S))
+    assert need >= 8 * 16 * 4 and call(ws_bytes=need - 1) == -4
+
+
+def test_adapter_workspace_grows_with_the_batch(S):
+    """The workspace of a batch covers 1 to 16 slices of M x R fp32 sums, whatever the sizes."""
+    for M in (1, 2, 15, 16, 17, 63, 64, 127, 128, 2048, 100000):
+        for count in (1, 3, 64, 1024):
+            for K in (32, 512, 5120, 25600):
+                for R in (8, 16, 40, 64, 72, 128):
+                    n = S.spense_adapters_workspace_size(M, pool(S, count=count, K=K, R=R))
+                    assert n % (M * R * 4) == 0 and 1 <= n // (M * R * 4) <= min(16, max(1, -(-K // 512)))
