@@ -645,6 +645,32 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
                         int64_t ldb, void* Y, int64_t ldy, uint32_t out_flags, void* ws, size_t ws_bytes,
                         hipStream_t stream);
 
+/*
+ * Products grouped by expert: for every position p of expert e (offsets, order as written by
+ * spense_group_rows over count experts),
+ *   Y[i][p, :] = round((X[row(p), :] W_{i,e}^T) * w_scales[i][e, :] * x_scale[row(p)]),
+ *   row(p) = order[p] / top (order NULL: p), for each of one or two weights i (gate and up),
+ * in one launch: the linear layer of sec. 3.2 for experts that each take the rows routed to them,
+ * ragged groups of any sizes, none read on the host.  With the T x top choices of T tokens grouped as
+ * T * top entries, row(p) is the token of position p.  Positions from offsets[count] on (rows of
+ * no expert) are left as they are.
+ * packed[i]: the first expert's weight, fp8 e4m3fn in the tiled layout, output- or input-split;
+ * expert e's values, meta and dense buffers follow at e times the sizes of spense_tiled_layout.
+ * Two weights share N, K, split and dense_begin.  w_scales: array of `weights` pointers to count x N
+ * fp32 (entries or the array may be NULL: ones); x_scale: rows_x fp32 or NULL.  X: rows_x x K
+ * fp8 codes, leading dimension ldx.  Y[i]: n x N, bf16 or fp32 (SPENSE_OUT_F32), leading
+ * dimension ldy[i].  fp32 sums whose order depends on the sizes only, rounded once.
+ * order entries whose row is outside [0, rows_x) give zeros, offsets are clamped to [0, n].
+ * Asynchronous, allocates nothing.  SPENSE_ERR_ARG for NULL pointers, weights outside [1, 2],
+ * count outside [1, SPENSE_MAX_GROUPS], top below 1, bad sizes or flags, mixed or unsupported
+ * weights, K = 0, ld below the row length, an X or one expert's buffer of 2 GiB or more;
+ * SPENSE_ERR_ALIGN for a misaligned X, Y or weight.
+ */
+int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order, int32_t top,
+                        const int32_t* offsets, int64_t n, int32_t count, int32_t weights,
+                        const spense_packed_t* const* packed, const float* const* w_scales, void* const* Y,
+                        const int64_t* ldy, uint32_t out_flags, hipStream_t stream);
+
 /* Thread-local description of the last error raised on this thread ("" if none). */
 const char* spense_last_error(void);
 

@@ -50,7 +50,7 @@ EXPORTS = ["spense_abi_version", "spense_set_log", "spense_last_error", "spense_
            "spense_obs_prune_workspace_size", "spense_obs_prune_24", "spense_gemm_grouped", "spense_gemm_glu",
            "spense_gemm_glu_pays", "spense_gemm_glu_fp8_workspace_size", "spense_gemm_glu_fp8", "spense_gemm_planned_workspace_size",
            "spense_gemm_planned", "spense_gemm_noalloc", "spense_block_norm", "spense_group_rows", "spense_combine_rows",
-           "spense_adapters_workspace_size", "spense_add_adapters"]
+           "spense_adapters_workspace_size", "spense_add_adapters", "spense_gemm_experts"]
 
 
 class SpenseError(RuntimeError):
@@ -159,6 +159,7 @@ def _load():
         "spense_adapters_workspace_size": (sz, [i64, P(spense_adapters_t)]),
         "spense_add_adapters": (ctypes.c_int, [p, i32, i64, i64, p, p, p, P(spense_adapters_t), p, i32, i64, p, i64,
                                                u32, p, sz, p]),
+        "spense_gemm_experts": (ctypes.c_int, [p, i64, i64, p, p, i32, p, i64, i32, i32, p, p, p, p, u32, p]),
         "spense_gemm_planned": (ctypes.c_int, [p, i64, i64, P(spense_packed_t), p, p, p, i64, u32, p, sz,
                                                P(spense_plan_override_t), p]),
     }
@@ -341,6 +342,12 @@ def spense_add_adapters(X, x_type, M, ldx, x_scale, order, offsets, pool: spense
                         ldy, out_flags, ws, ws_bytes, stream) -> int:
     return _lib.spense_add_adapters(X, x_type, M, ldx, x_scale, order, offsets, ctypes.byref(pool), base, base_type,
                                     ldb, Y, ldy, out_flags, ws, ws_bytes, stream)
+
+
+def spense_gemm_experts(X, rows_x, ldx, x_scale, order, top, offsets, n, count, weights, packed_array, w_scales_array,
+                        Y_array, ldy_array, out_flags, stream) -> int:
+    return _lib.spense_gemm_experts(X, rows_x, ldx, x_scale, order, top, offsets, n, count, weights, packed_array,
+                                    w_scales_array, Y_array, ldy_array, out_flags, stream)
 
 
 # ------------------------------------------------------------------ torch helpers
@@ -891,6 +898,11 @@ def _ld(t):
     return max(t.stride(0), t.shape[1])
 
 
+def _ld16(t):
+    """The same for rows that must start 16 bytes apart (bytes)."""
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+
+
 def block_norm(x: torch.Tensor, y: torch.Tensor | None = None, *, post_weight=None, gate=None,
                residual_scale: float = 1.0, weight=None, eps: float = 1e-6, quantize: bool = True,
                normed: bool = False, residual_out=None, normed_out=None, codes_out=None, scales_out=None) -> BlockNorm:
@@ -1075,3 +1087,99 @@ def gemm_adapters(X: torch.Tensor, pw: PackedWeight, pool: AdapterPool, groups: 
         X, x_scale = A_x, None
     return add_adapters(base, X, pool, groups, x_scale, out=base if out_f32 and out is None else out, out_f32=out_f32,
                         workspace=workspace)
+
+
+# ------------------------------------------------------------------ products grouped by expert
+class PackedExperts:
+    """One fp8 weight per expert, all of one geometry, in the tiled layout: the experts' buffers one
+    after the other (values, meta, dense: count rows each) and the first expert's descriptor."""
+
+    def __init__(self, count, N, K, split, dense_begin, values, meta, dense):
+        self.count, self.N, self.K, self.split, self.dense_begin = count, N, K, split, dense_begin
+        self.values, self.meta, self.dense = values, meta, dense
+        self.device = dense.device
+        L = spense_layout(N, K, SPENSE_FP8_E4M3FN, split, dense_begin)
+        self.desc = spense_packed_t(SPENSE_FP8_E4M3FN, split, N, K, dense_begin, _ptr(values), L.values_ld, _ptr(meta),
+                                    L.meta_ld, _ptr(dense), L.dense_ld, SPENSE_LAYOUT_TILED)
+
+
+def stack_experts(pws) -> PackedExperts:
+    """The experts' tiled fp8 weights (``tile``) as gemm_experts takes them: copied one after the other."""
+    pws = list(pws)
+    if not pws:
+        raise ValueError("at least one expert")
+    p0 = pws[0]
+    for p in pws:
+        if p.kind != SPENSE_LAYOUT_TILED or p.dtype != SPENSE_FP8_E4M3FN:
+            raise ValueError("experts' weights must be fp8 in the tiled layout (tile)")
+        if (p.N, p.K, p.split, p.dense_begin) != (p0.N, p0.K, p0.split, p0.dense_begin):
+            raise ValueError("experts' weights must have one N, K, split and dense_begin")
+    return PackedExperts(len(pws), p0.N, p0.K, p0.split, p0.dense_begin, torch.stack([p.values for p in pws]),
+                         torch.stack([p.meta for p in pws]), torch.stack([p.dense for p in pws]))
+
+
+def gemm_experts(X: torch.Tensor, experts, groups: RowGroups, w_scales=None, x_scale=None, *, top: int = 1,
+                 gathered: bool = False, outs=None, out_f32: bool = False):
+    """Y_i[p] = X[row(p)] W_{i,e}^T for every position p of every expert e (spense_gemm_experts), one
+    launch for one or two weights (a list of PackedExperts of one geometry, e.g. [gate, up]); returns the
+    list of outputs, n x N each, in the positions of ``groups`` (group_rows over the experts).  X holds
+    one row per token, row(p) = order[p] // top; with ``gathered`` X's rows are the positions
+    themselves.  w_scales: count x N fp32 per weight.  Rows of positions in no group are not written."""
+    experts = list(experts)
+    k = len(experts)
+    if k not in (1, 2):
+        raise ValueError("one or two weights")
+    e0 = experts[0]
+    _check_x(X, SPENSE_FP8_E4M3FN, e0.K)
+    if top < 1:
+        raise ValueError(f"top = {top}")
+    n, dev = groups.n, X.device
+    for w in experts:
+        if groups.groups != w.count:
+            raise ValueError(f"groups are over {groups.groups} experts, the weights over {w.count}")
+        _on_gpu(dev, experts=w.dense)
+    if X.shape[0] * (1 if gathered else top) != n:
+        raise ValueError(f"X has {X.shape[0]} rows, the groups {n}")
+    if w_scales is None:
+        w_scales = [None] * k
+    if len(w_scales) != k:
+        raise ValueError("one w_scale per weight")
+    for w, s in zip(experts, w_scales):
+        if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (w.count, w.N) or not s.is_contiguous()
+                              or s.device != dev):
+            raise ValueError(f"w_scale must be a contiguous fp32 tensor of shape {(w.count, w.N)} on {dev}")
+    _check_scale(x_scale, X.shape[0], dev, "x_scale")
+    _on_gpu(dev, groups=groups.order)
+    if outs is None:
+        outs = [None] * k
+    if len(outs) != k:
+        raise ValueError("one output per weight")
+    outs = [_out(o, n, w.N, out_f32, dev, f"outs[{i}]") for i, (o, w) in enumerate(zip(outs, experts))]
+    parr = (ctypes.POINTER(spense_packed_t) * k)(*[ctypes.pointer(w.desc) for w in experts])
+    sarr = (ctypes.c_void_p * k)(*[_ptr(s) for s in w_scales])
+    yarr = (ctypes.c_void_p * k)(*[_ptr(o) for o in outs])
+    larr = (ctypes.c_int64 * k)(*[_ld(o) for o in outs])
+    with _device(dev):
+        _check(spense_gemm_experts(_ptr(X), X.shape[0], _ld16(X), _ptr(x_scale), None if gathered else _ptr(groups.order),
+                                   top, _ptr(groups.offsets), n, e0.count, k, parr, sarr, yarr, larr,
+                                   SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, _stream(dev)))
+    return outs
+
+
+def mlp_experts(X: torch.Tensor, x_scale: torch.Tensor, idx: torch.Tensor, weights: torch.Tensor, gate: PackedExperts,
+                up: PackedExperts, down: PackedExperts, gate_scale=None, up_scale=None, down_scale=None, out=None,
+                out_f32: bool = False) -> torch.Tensor:
+    """A GLU MLP of experts (``mlp`` of each token's choices, summed): idx T x top int32 names each
+    token's experts (outside [0, count): none), weights T x top fp32 what each counts.  The rows are
+    grouped by expert, gate and up computed for every position, H = up * silu(gate) quantised per row,
+    down computed and each token's rows summed in fp32.  X: T x K fp8 codes with x_scale."""
+    if idx.dim() != 2 or idx.shape[0] != X.shape[0] or weights.shape != idx.shape:
+        raise ValueError("idx and weights must be T x top")
+    top = idx.shape[1]
+    if top < 1:
+        raise ValueError("at least one expert per token")
+    groups = group_rows(idx.reshape(-1), gate.count)
+    G, U = gemm_experts(X, [gate, up], groups, [gate_scale, up_scale], x_scale, top=top, out_f32=True)
+    Hq, sh = glu_quantize_fp8(G, U)
+    D, = gemm_experts(Hq, [down], groups, [down_scale], sh, gathered=True, out_f32=True)
+    return combine_rows(D, groups, weights, top, out=out, out_f32=out_f32)

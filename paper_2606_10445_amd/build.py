@@ -16,6 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspense.so")
 SOURCES = ["spense_api.cpp", "spense_gemm.hip", "spense_gemm_big2.hip", "spense_gemm_mid.hip", "spense_compress.hip", "spense_quant.hip",
            "spense_index.hip", "spense_obs.hip", "spense_norm.hip", "spense_groups.hip", "spense_adapters.hip",
+           "spense_experts.hip",
            "spense_noalloc.hip"]
 ARCH = "gfx950"
 

@@ -1,0 +1,280 @@
+// Products grouped by expert on Spense weights: Y[p] = X[row(p)] W_e^T for the positions p of
+// expert e (spense_group_rows), ragged groups of any size, one or two weights per expert (gate
+// and up) in one launch.  Nothing of the grouping is read on the host.
+//
+// Few rows an expert (decoding): the weights of the experts that got rows are the traffic, 0.625
+// byte a 2:4 entry and one a dense entry.  experts_rows_kernel streams them once per tile of 16,
+// 32 or 64 positions: a wave owns 16 weight rows over all of K and keeps two or three chunks of
+// 512 columns in registers ahead of the one in its matrix instructions; the tile's activations,
+// gathered row by row, go through LDS a chunk at a time, shared by the workgroup's waves.
+// Many rows: the 128 x 128 kernel over tiles of positions (spense_gemm_mid.hip).
+#include <cstring>
+
+#include "spense_gemm_device.h"
+#include "spense_rows_device.h"
+
+namespace spense {
+namespace {
+
+// A region of one weight as the row-split kernel sees it: its 16-row tiles from `tile0` on.
+struct ExpertRegion {
+  int32_t tile0, row0, rows, mat;
+  int32_t n_sp, n_de;  // chunks of 512 columns, 2:4 then dense
+};
+
+struct ExpertArgs {
+  const uint8_t* X;
+  int64_t ldx_b;
+  uint32_t x_bytes;
+  const float* sx;
+  int32_t K, kbound;  // kbound: the first dense column of an input-split weight, 0 of an output-split one
+  int32_t out_f32;
+  int32_t tiles, wgs;  // 16-row tiles of all regions, workgroups of a tile of positions
+  int32_t nreg;
+  ExpertRegion reg[4];
+  MatDesc mat[2];
+};
+
+template <int CT, int WV>
+__global__ __launch_bounds__(64 * WV) void experts_rows_kernel(ExpertArgs a, ExpertRows er) {
+  typedef XTile<kFP8, CT> XT;
+  constexpr int NS = CT <= 2 ? 4 : 3, D = NS - 1, P = CT == 1 ? 4 : 1;
+  constexpr int KC = XT::CHUNK_K, XI = XT::BYTES / 1024 / WV, NL = 9;  // loads a chunk: activations, weights
+  static_assert(XI >= 1 && XI * 1024 * WV == XT::BYTES, "an activation chunk splits evenly over the waves");
+  RowTile t;
+  if (!find_tile(er.offsets, er.count, er.n, false, 16 * CT, blockIdx.x / a.wgs, t)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, li = lane & 15, lq = lane >> 4;
+  const int tile = (blockIdx.x % a.wgs) * WV + wave;
+  const bool active = tile < a.tiles;
+  int ri = 0;
+  for (int i = 1; i < a.nreg; ++i)
+    if (tile >= a.reg[i].tile0) ri = i;
+  const ExpertRegion& R = a.reg[ri];
+  const MatDesc& MD = a.mat[R.mat];
+  const int rt = tile - R.tile0, nbase = R.row0 + 16 * rt, rowend = R.row0 + R.rows;
+  const int64_t e = t.group;
+  __shared__ __attribute__((aligned(1024))) uint8_t xbuf[NS][XT::BYTES];
+  const __amdgpu_buffer_rsrc_t rx = rsrc(a.X, a.x_bytes), rv = rsrc(MD.values + e * MD.v_bytes, MD.v_bytes),
+                               rm = rsrc(reinterpret_cast<const uint8_t*>(MD.meta) + e * MD.m_bytes, MD.m_bytes),
+                               rd = rsrc(MD.dense + e * MD.d_bytes, MD.d_bytes);
+  // this lane's 16 bytes of each activation block it copies: tile row and column, swizzled as XTile says
+  uint32_t xo[XI];
+#pragma unroll
+  for (int i = 0; i < XI; ++i) {
+    const int byte = (wave * XI + i) * 1024 + 16 * lane, r = byte / XT::ROW_B, b = ((byte % XT::ROW_B) >> 4) ^ (r & 31);
+    const int src = t.p0 + r < t.p1 ? source_row(er, t.p0 + r) : -1;
+    xo[i] = src >= 0 ? (uint32_t)((int64_t)src * a.ldx_b) + 16u * b : kOOB;
+  }
+  // the output's scales, requested before any weight
+  EpiScales<1, CT> es;
+  if (active) {
+    epi_scales(es, MD.sw ? MD.sw + e * er.N : nullptr, nullptr, er.n, nbase + 4 * lq, t.p0 + li, rowend);
+    source_scales<CT>(es.x, er, a.sx, t.p0 + li, t.p1);
+  }
+  v4f acc[1][CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) acc[0][c] = (v4f){0.f, 0.f, 0.f, 0.f};
+
+  // chunks of the workgroup: [0, kbound) then [kbound, K), 512 columns each; an output-split
+  // region is of one kind over all of them
+  const int nb = (a.kbound + KC - 1) / KC, chunks = nb + (a.K - a.kbound + KC - 1) / KC;
+  const uint32_t vt = (uint32_t)rt * (uint32_t)R.n_sp * 4096u + 16u * lane, mt = (uint32_t)rt * (uint32_t)R.n_sp * 1024u + 16u * lane,
+                 dt = (uint32_t)rt * (uint32_t)R.n_de * 8192u + 16u * lane;
+  auto load = [&](WChunk& W, int c) {
+    load_chunk_tiled(W, c < R.n_sp, c < chunks, c, max(c - R.n_sp, 0), vt, mt, dt, rv, rm, rd);
+  };
+  auto xload = [&](int buf, int c) {
+    const int kc = c < nb ? c * KC : a.kbound + (c - nb) * KC, ke = c >= chunks ? -1 : c < nb ? a.kbound : a.K;
+#pragma unroll
+    for (int i = 0; i < XI; ++i) {
+      const int byte = (wave * XI + i) * 1024 + 16 * lane, r = byte / XT::ROW_B, b = ((byte % XT::ROW_B) >> 4) ^ (r & 31);
+      lds_load16<0>(rx, xbuf[buf] + (wave * XI + i) * 1024, kc + 16 * b < ke ? xo[i] : kOOB, max(kc, 0));
+    }
+  };
+  // the pipeline of spense_gemm_rows_kernel: chunk c + D requested in step c, the barrier after
+  // it waits for the activations of chunk c + 1 only
+  auto run = [&](auto act_const) {
+    constexpr bool ACT = decltype(act_const)::value;
+    constexpr int AFTER = ACT ? NL + (D - 1) * (XI + NL) : (D - 1) * XI;
+    WChunk slot[NS][1];
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      xload(d, d);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (ACT) load(slot[d][0], d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    barrier_vm<AFTER>();
+    auto step = [&](auto s_const, int c) {
+      constexpr int S = decltype(s_const)::value, SD = (S + D) % NS;
+      xload(SD, c + D);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (ACT) {
+        load(slot[SD][0], c + D);
+        __builtin_amdgcn_sched_barrier(0);
+        mma_chunk<kFP8, CT, 1, true, P>(acc, slot[S], c < R.n_sp, xbuf[S], li, lq);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      barrier_vm<AFTER>();
+    };
+    int c = 0;
+    for (; c + NS <= chunks; c += NS) static_for<NS>([&](auto s_const) { step(s_const, c + decltype(s_const)::value); });
+    static_for<NS - 1>([&](auto s_const) {
+      if (c + decltype(s_const)::value < chunks) step(s_const, c + decltype(s_const)::value);
+    });
+  };
+  if (active)
+    run(std::true_type());
+  else
+    run(std::false_type());
+  if (!active) return;
+  xdl_fence();
+  GemmArgs o;
+  o.out_f32 = a.out_f32;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int p = t.p0 + 16 * c + li, n0 = nbase + 4 * lq;
+    if (p < t.p1 && n0 < rowend) store4e(MD.Y, MD.ldy, MD.sw != nullptr, MD.vec_store, o, es, 0, c, acc[0][c], p, n0, rowend);
+  }
+}
+
+}  // namespace
+}  // namespace spense
+
+using spense::api_fail;
+
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace
+
+extern "C" int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order,
+                                   int32_t top, const int32_t* offsets, int64_t n, int32_t count, int32_t weights,
+                                   const spense_packed_t* const* packed, const float* const* w_scales, void* const* Y,
+                                   const int64_t* ldy, uint32_t out_flags, hipStream_t stream) {
+  if (weights < 1 || weights > 2) return api_fail(SPENSE_ERR_ARG, "weights=%d outside [1, 2]", weights);
+  if (count < 1 || count > SPENSE_MAX_GROUPS)
+    return api_fail(SPENSE_ERR_ARG, "count=%d outside [1, %d]", count, SPENSE_MAX_GROUPS);
+  if (!packed || !Y || !ldy) return api_fail(SPENSE_ERR_ARG, "NULL array");
+  if (n < 0 || n > INT32_MAX || rows_x < 0 || rows_x > INT32_MAX)
+    return api_fail(SPENSE_ERR_ARG, "bad n=%lld rows_x=%lld", (long long)n, (long long)rows_x);
+  if (top < 1) return api_fail(SPENSE_ERR_ARG, "top=%d", top);
+  if (out_flags & ~1u) return api_fail(SPENSE_ERR_ARG, "unknown out_flags 0x%x", out_flags);
+  const int64_t out_es = (out_flags & SPENSE_OUT_F32) ? 4 : 2;
+  for (int i = 0; i < weights; ++i) {
+    if (!packed[i]) return api_fail(SPENSE_ERR_ARG, "packed[%d] is NULL", i);
+    int rc = spense::api_check_packed(packed[i]);
+    if (rc) return rc;
+    const spense_packed_t& P = *packed[i];
+    if (P.dtype != SPENSE_FP8_E4M3FN || P.layout != SPENSE_LAYOUT_TILED)
+      return api_fail(SPENSE_ERR_ARG, "experts' weights must be fp8 in the tiled layout");
+    if (P.N != packed[0]->N || P.K != packed[0]->K || P.split != packed[0]->split || P.dense_begin != packed[0]->dense_begin)
+      return api_fail(SPENSE_ERR_ARG, "the two weights must have one geometry");
+  }
+  const spense_packed_t& P = *packed[0];
+  const int64_t N = P.N, K = P.K;
+  if (n == 0 || N == 0) return spense::api_ok();
+  if (K < 1) return api_fail(SPENSE_ERR_ARG, "K=0");
+  if (!X || !offsets) return api_fail(SPENSE_ERR_ARG, "X or offsets is NULL");
+  if (ldx < K) return api_fail(SPENSE_ERR_ARG, "ldx=%lld < K=%lld", (long long)ldx, (long long)K);
+  if (reinterpret_cast<uintptr_t>(X) % 16 || ldx % 16)
+    return api_fail(SPENSE_ERR_ALIGN, "X must be 16-byte aligned with a 16-byte multiple row pitch");
+  for (int i = 0; i < weights; ++i) {
+    if (!Y[i]) return api_fail(SPENSE_ERR_ARG, "Y[%d] is NULL", i);
+    if (ldy[i] < N) return api_fail(SPENSE_ERR_ARG, "ldy[%d] < N", i);
+    if (reinterpret_cast<uintptr_t>(Y[i]) % out_es) return api_fail(SPENSE_ERR_ALIGN, "Y[%d] misaligned", i);
+    if (n * ldy[i] > (int64_t)1 << 40) return api_fail(SPENSE_ERR_ARG, "Y[%d] too large", i);
+  }
+  const int64_t lim = (int64_t)1 << 31;
+  const int64_t xb = rows_x > 0 ? (rows_x - 1) * ldx + K : 0;
+  if (xb >= lim) return api_fail(SPENSE_ERR_ARG, "X spans 2 GiB or more");
+  spense_tiled_layout_t T;
+  int rc = spense_tiled_layout(N, K, P.dtype, P.split, P.dense_begin, &T);
+  if (rc) return rc;
+  if ((int64_t)T.values_bytes >= lim || (int64_t)T.meta_bytes >= lim || (int64_t)T.dense_bytes >= lim)
+    return api_fail(SPENSE_ERR_ARG, "an expert's weight spans 2 GiB or more");
+  const bool in_split = P.split == SPENSE_SPLIT_INPUT;
+  const int64_t db = P.dense_begin;
+  // regions: the dense rows of every weight first (their workgroups carry more bytes), then the 2:4 rows
+  struct {
+    int64_t row0, rows, kbound;
+    int mat;
+  } reg[4];
+  int nreg = 0;
+  for (int kind = 0; kind < (in_split ? 1 : 2); ++kind)
+    for (int i = 0; i < weights; ++i) {
+      if (in_split)
+        reg[nreg++] = {0, N, db, i};
+      else if (kind == 0 && N > db)
+        reg[nreg++] = {db, N - db, 0, i};
+      else if (kind == 1 && db > 0)
+        reg[nreg++] = {0, db, K, i};
+    }
+  spense::MatDesc mat[2];
+  bool vec_rows = in_split || db % 4 == 0;
+  for (int i = 0; i < weights; ++i)
+    mat[i] = spense::MatDesc{static_cast<const uint8_t*>(packed[i]->values), packed[i]->meta,
+                             static_cast<const uint8_t*>(packed[i]->dense), (uint32_t)T.values_bytes, (uint32_t)T.meta_bytes,
+                             (uint32_t)T.dense_bytes, Y[i], ldy[i], w_scales ? w_scales[i] : nullptr,
+                             vec_rows && ldy[i] % 4 == 0 && reinterpret_cast<uintptr_t>(Y[i]) % (4 * out_es) == 0};
+  spense::ExpertRows er;
+  memset(&er, 0, sizeof er);
+  er.order = order, er.offsets = offsets, er.n = (int32_t)n, er.count = count, er.top = top, er.rows_x = (int32_t)rows_x;
+  er.N = (int32_t)N;
+  const int64_t avg = n / (count < n ? count : n);
+  hipError_t e;
+  if (avg >= 48) {
+    spense::GemmArgs g;
+    memset(&g, 0, sizeof g);
+    g.X = static_cast<const uint8_t*>(X), g.ldx_b = ldx, g.x_bytes = (uint32_t)xb, g.sx = x_scale;
+    g.M = (int32_t)n, g.N = (int32_t)N, g.out_f32 = (out_flags & SPENSE_OUT_F32) ? 1 : 0;
+    g.tiled = 1, g.tblocks = 1, g.nmat = weights, g.nreg = nreg;
+    for (int i = 0; i < weights; ++i) g.mat[i] = mat[i];
+    int64_t blocks = 0;
+    for (int i = 0; i < nreg; ++i) {
+      spense::Region& R = g.reg[i];
+      R.row0 = (int32_t)reg[i].row0, R.rows = (int32_t)reg[i].rows, R.kbound = (int32_t)reg[i].kbound, R.kend = (int32_t)K;
+      R.dense_row_off = in_split ? 0 : (int32_t)db, R.dense_col_off = in_split ? (int32_t)db : 0;
+      R.ksplit = 1, R.mat = reg[i].mat, R.wg0 = (int32_t)blocks, R.nrb = (int32_t)ceil_div(reg[i].rows, 128);
+      blocks += R.nrb;
+    }
+    g.groups = (int32_t)blocks;
+    er.row_blocks = (int32_t)(ceil_div(blocks, 8) * 8);
+    if (spense::most_tiles(n, count, false, 128) * er.row_blocks > INT32_MAX)
+      return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
+    rc = spense::api_check_device();
+    if (rc) return rc;
+    e = spense::launch_experts_mid(g, er, stream);
+  } else {
+    spense::ExpertArgs a;
+    memset(&a, 0, sizeof a);
+    a.X = static_cast<const uint8_t*>(X), a.ldx_b = ldx, a.x_bytes = (uint32_t)xb, a.sx = x_scale;
+    a.K = (int32_t)K, a.kbound = in_split ? (int32_t)db : 0, a.out_f32 = (out_flags & SPENSE_OUT_F32) ? 1 : 0;
+    a.nreg = nreg;
+    for (int i = 0; i < weights; ++i) a.mat[i] = mat[i];
+    int64_t tiles = 0;
+    for (int i = 0; i < nreg; ++i) {
+      a.reg[i] = {(int32_t)tiles, (int32_t)reg[i].row0, (int32_t)reg[i].rows, reg[i].mat, (int32_t)ceil_div(reg[i].kbound, 512),
+                  (int32_t)ceil_div(K - reg[i].kbound, 512)};
+      tiles += ceil_div(reg[i].rows, 16);
+    }
+    a.tiles = (int32_t)tiles;
+    const int ct = avg <= 12 ? 1 : avg <= 24 ? 2 : 4, wv = ct == 1 ? 4 : 8;
+    a.wgs = (int32_t)ceil_div(tiles, wv);
+    const int64_t grid = spense::most_tiles(n, count, false, 16 * ct) * a.wgs;
+    if (grid > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
+    rc = spense::api_check_device();
+    if (rc) return rc;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * wv), 0, stream, a, er); };
+    if (ct == 1)
+      go(spense::experts_rows_kernel<1, 4>);
+    else if (ct == 2)
+      go(spense::experts_rows_kernel<2, 8>);
+    else
+      go(spense::experts_rows_kernel<4, 8>);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) return api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));
+  return spense::api_ok();
+}

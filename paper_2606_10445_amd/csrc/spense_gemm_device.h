@@ -82,6 +82,156 @@ __device__ __forceinline__ v4f mma_dense(v8i a, v8i b, v4f c, std::integral_cons
                                                  0, 0);
 }
 
+// ---------------------------------------------------------------- chunks of the row-split kernels
+// A chunk of activations in LDS (16 * CT rows of 512 bytes, 16-byte blocks XOR-swizzled by row),
+// a chunk of one row tile's weights in registers, and the chunk's MMAs.
+template <int DT, int CT>
+struct XTile {
+  static constexpr int KS = Traits<DT>::KS;
+  static constexpr int CHUNK_K = 4 * KS;                  // logical K per chunk
+  static constexpr int ROW_B = CHUNK_K * Traits<DT>::ES;  // bytes per activation row (512)
+  static constexpr int ROWS = 16 * CT;
+  static constexpr int BYTES = ROWS * ROW_B;
+  // LDS byte address of 16-byte block b of row r
+  __device__ static __forceinline__ int addr(int r, int b) { return r * ROW_B + ((b ^ (r & 31)) << 4); }
+};
+
+template <int DT, int CT>
+__device__ __forceinline__ v4i xlds(const uint8_t* lds, int r, int byte) {
+  return *reinterpret_cast<const v4i*>(lds + XTile<DT, CT>::addr(r, byte >> 4) + (byte & 15));
+}
+
+// B fragments of one step from the LDS tile (step_b: byte offset of the step in a row).
+// 2:4 steps and dense fp8 steps read K [16q, 16q+16) and [64+16q, 64+16q+16) of the
+// step; dense bf16 steps read K [8q, 8q+8).
+template <int DT, int CT>
+__device__ __forceinline__ void frag_pair(v8i (&b)[CT], const uint8_t* lds, int li, int lq, int step_b) {
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int r = 16 * c + li;
+    b[c] = cat8(xlds<DT, CT>(lds, r, step_b + 16 * lq), xlds<DT, CT>(lds, r, step_b + 64 + 16 * lq));
+  }
+}
+template <int DT, int CT>
+__device__ __forceinline__ void frag_one(v8i (&b)[CT], const uint8_t* lds, int li, int lq, int step_b) {
+  const v4i z = {0, 0, 0, 0};
+#pragma unroll
+  for (int c = 0; c < CT; ++c) b[c] = cat8(xlds<DT, CT>(lds, 16 * c + li, step_b + 16 * lq), z);
+}
+
+// Weights of one chunk in registers: eight 16-byte fragments and four metadata words.
+// fp8 (both kinds of chunk have four 128-wide steps): w[j] is step j's 2:4 value fragment
+// or the first half of its dense fragment, w[4+j] the dense second half.  bf16: w[j] is
+// step j's value fragment (2:4, j < 4) or dense fragment (eight 32-wide steps).
+struct WChunk {
+  v4i w[8];
+  int ix[4];
+};
+
+// Tiled layout (fp8): each fragment of the chunk is one contiguous kilobyte.  vt, mt, dt:
+// this lane's byte offset in its tile's first 2:4 / metadata / dense chunk (16 * lane
+// included); cs, cd >= 0: the chunk's index within the 2:4 / dense part.  The chunk part
+// of the address travels in the scalar offset; ok = false masks every lane.
+__device__ __forceinline__ void load_chunk_tiled(WChunk& W, bool sparse, bool ok, int cs, int cd, uint32_t vt,
+                                                 uint32_t mt, uint32_t dt, __amdgpu_buffer_rsrc_t rv,
+                                                 __amdgpu_buffer_rsrc_t rm, __amdgpu_buffer_rsrc_t rd) {
+  const __amdgpu_buffer_rsrc_t rw = sparse ? rv : rd;
+  const uint32_t base = sel(ok, sparse ? vt : dt);
+  const uint32_t dbase = sel(ok && !sparse, dt);
+  const int s0 = sparse ? cs * 4096 : cd * 8192, sj = sparse ? 1024 : 2048;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    W.w[j] = bl16<kTiledNT>(rw, base, s0 + sj * j);
+    W.w[4 + j] = bl16<kTiledNT>(rd, dbase, cd * 8192 + 2048 * j + 1024);
+  }
+  const v4i w = bl16<kTiledNT>(rm, sel(ok && sparse, mt), cs * 1024);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) W.ix[j] = w[j];
+}
+
+// The metadata word of each step for this lane group.  Wide loads: lane group q holds
+// step q's four words; a 4x4 transpose across lane groups (two lane swaps) gives lane
+// group q word 4j+q of every step j.
+template <bool WM>
+__device__ __forceinline__ void meta_words(int (&ix)[4], const WChunk& W) {
+  if constexpr (WM) {
+    const auto s02 = __builtin_amdgcn_permlane32_swap((unsigned)W.ix[0], (unsigned)W.ix[2], false, false);
+    const auto s13 = __builtin_amdgcn_permlane32_swap((unsigned)W.ix[1], (unsigned)W.ix[3], false, false);
+    const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
+    const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
+    ix[0] = (int)s01[0];
+    ix[1] = (int)s01[1];
+    ix[2] = (int)s23[0];
+    ix[3] = (int)s23[1];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ix[j] = W.ix[j];
+  }
+}
+
+// MMAs of one chunk.  The B fragments of P steps are read from LDS before their MMAs,
+// so the LDS latency is paid once per group rather than once per step.
+template <int DT, int CT, int RT, bool WM, int P>
+__device__ __forceinline__ void mma_chunk(v4f (&acc)[RT][CT], const WChunk (&W)[RT], bool sparse, const uint8_t* lds,
+                                          int li, int lq) {
+  static_assert(P == 1 || P == 2 || P == 4, "fragment group size");
+  // each B fragment read from LDS feeds the RT row tiles of this wave
+  if (sparse) {
+    int mw[RT][4];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) meta_words<WM>(mw[t], W[t]);
+#pragma unroll
+    for (int j0 = 0; j0 < 4; j0 += P) {
+      v8i b[P][CT];
+#pragma unroll
+      for (int j = 0; j < P; ++j) frag_pair<DT, CT>(b[j], lds, li, lq, (j0 + j) * 128);
+      if constexpr (P > 1) __builtin_amdgcn_sched_barrier(0);  // all reads of the group before its MMAs
+#pragma unroll
+      for (int j = 0; j < P; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const int ix = DT == kFP8 ? mw[t][j0 + j] : (int)((uint32_t)mw[t][j0 + j] >> (16 * (lq & 1)));
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+            acc[t][c] = mma_sparse(W[t].w[j0 + j], b[j][c], acc[t][c], ix, std::integral_constant<int, DT>());
+        }
+    }
+  } else if constexpr (DT == kFP8) {
+#pragma unroll
+    for (int j0 = 0; j0 < 4; j0 += P) {
+      v8i b[P][CT];
+#pragma unroll
+      for (int j = 0; j < P; ++j) frag_pair<DT, CT>(b[j], lds, li, lq, (j0 + j) * 128);
+      if constexpr (P > 1) __builtin_amdgcn_sched_barrier(0);  // all reads of the group before its MMAs
+#pragma unroll
+      for (int j = 0; j < P; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const v8i av = cat8(W[t].w[j0 + j], W[t].w[4 + j0 + j]);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[t][c] = mma_dense(av, b[j][c], acc[t][c], std::integral_constant<int, DT>());
+        }
+    }
+  } else {
+    const v4i z = {0, 0, 0, 0};
+#pragma unroll
+    for (int j0 = 0; j0 < 8; j0 += 2 * P) {
+      v8i b[2 * P][CT];
+#pragma unroll
+      for (int j = 0; j < 2 * P; ++j) frag_one<DT, CT>(b[j], lds, li, lq, (j0 + j) * 64);
+      if constexpr (P > 1) __builtin_amdgcn_sched_barrier(0);  // all reads of the group before its MMAs
+#pragma unroll
+      for (int j = 0; j < 2 * P; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const v8i av = cat8(W[t].w[j0 + j], z);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[t][c] = mma_dense(av, b[j][c], acc[t][c], std::integral_constant<int, DT>());
+        }
+    }
+  }
+}
+
 // ---------------------------------------------------------------- epilogue
 __device__ __forceinline__ uint32_t bf16_bits(float v) {
   __bf16 h = (__bf16)v;  // round to nearest even

@@ -1,5 +1,6 @@
 // The 128-row large-M kernel (spense_gemm.hip has the overview of all GEMM kernels).
 #include "spense_gemm_device.h"
+#include "spense_rows_device.h"
 
 namespace spense {
 namespace {
@@ -37,8 +38,13 @@ namespace {
 constexpr int kMidRows = 128, kMidTok = 128, kMidX = kMidTok * 128, kMidStage = kMidX + 16384;
 constexpr int kMidStages = 5, kMidLds = kMidStages * kMidStage;
 
-template <int DT>
-__global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
+// RG: rows grouped by expert.  A workgroup's tokens are a tile of positions of one expert
+// (find_tile; positions past the last tile's end have no workgroup), its weight that expert's
+// (the experts' buffers one after the other), position p reads activation row order[p] / top and
+// writes output row p.  Workgroup 8 l + x takes row blocks x, x + 8, ... of one tile after the
+// other, so that a row block of an expert is read by one XCD only.
+template <int DT, bool RG>
+__device__ __forceinline__ void mid_body(const GemmArgs& a, const ExpertRows& er) {
   constexpr bool TL = DT == kFP8;  // tiled weights; bf16 reads the row-major layout
   constexpr int ES = Traits<DT>::ES;
   typedef std::integral_constant<int, DT> Dt;
@@ -50,7 +56,12 @@ __global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
   const int wr = wave & 3, wc = (wave >> 2) & 1;  // row quarter and token half of a computing wave
   const int cw = wave & 3;                        // number of a copying wave
   int g = blockIdx.x;
-  if (a.xgt > 0 && g < a.xg1) {  // XCD-aware order, as in the 256 x 256 kernel
+  RowTile rt = {0, 0, 0};
+  if constexpr (RG) {
+    const int per = er.row_blocks >> 3, x = g & 7, l = g >> 3;
+    g = (l % per) * 8 + x;
+    if (g >= a.groups || !find_tile(er.offsets, er.count, er.n, false, kMidTok, l / per, rt)) return;
+  } else if (a.xgt > 0 && g < a.xg1) {  // XCD-aware order, as in the 256 x 256 kernel
     const int T = a.tblocks, GT = a.xgt, RC = a.xrc, TGc = T / GT;
     const int x = g & 7, l = g >> 3, tg = x % TGc, rc = x / TGc;
     g = ((l / GT) * RC + rc) * T + tg * GT + l % GT;
@@ -61,7 +72,8 @@ __global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
   const Region& R = a.reg[ri];
   const int S = R.ksplit, rs = (g - R.wg0) / a.tblocks;
   const int rb = rs / S, slice = rs - rb * S;
-  const int m0 = (g - R.wg0) % a.tblocks * kMidTok;
+  const int m0 = RG ? rt.p0 : (g - R.wg0) % a.tblocks * kMidTok;
+  const int mend = RG ? rt.p1 : a.M;
   const int rowend = R.row0 + R.rows, rblk = R.row0 + rb * kMidRows;
   const int K = R.kend * ES, kbound = R.kbound * ES;  // bytes of an activation row
   const int n_sp = (kbound + 127) / 128, n_de = (K - kbound + 127) / 128;
@@ -74,8 +86,10 @@ __global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
 
   extern __shared__ __attribute__((aligned(1024))) uint8_t mid_lds[];
   const MatDesc& MD = a.mat[R.mat];
-  const __amdgpu_buffer_rsrc_t rx = rsrc(a.X, a.x_bytes), rv = rsrc(MD.values, MD.v_bytes), rm = rsrc(MD.meta, MD.m_bytes),
-                               rd = rsrc(MD.dense, MD.d_bytes);
+  const int64_t ex = RG ? rt.group : 0;
+  const __amdgpu_buffer_rsrc_t rx = rsrc(a.X, a.x_bytes), rv = rsrc(MD.values + ex * MD.v_bytes, MD.v_bytes),
+                               rm = rsrc(reinterpret_cast<const uint8_t*>(MD.meta) + ex * MD.m_bytes, MD.m_bytes),
+                               rd = rsrc(MD.dense + ex * MD.d_bytes, MD.d_bytes);
   v4f acc[RPW][TC];
 #pragma unroll
   for (int t = 0; t < RPW; ++t)
@@ -93,7 +107,12 @@ __global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
       const int m = m0 + 8 * (XL * cw + i) + (lane >> 3);
-      xo[i] = m < a.M ? (uint32_t)((int64_t)m * a.ldx_b + (xb ^ (64 * (i & 1)))) : kOOB;
+      if constexpr (RG) {
+        const int src = m < mend ? source_row(er, m) : -1;
+        xo[i] = src >= 0 ? (uint32_t)((int64_t)src * a.ldx_b + (xb ^ (64 * (i & 1)))) : kOOB;
+      } else {
+        xo[i] = m < a.M ? (uint32_t)((int64_t)m * a.ldx_b + (xb ^ (64 * (i & 1)))) : kOOB;
+      }
     }
     if constexpr (TL) {
 #pragma unroll
@@ -276,7 +295,7 @@ __global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
     loop(std::true_type(), ns);
     loop(std::false_type(), n);
   };
-  const bool idle = copies || m0 + 16 * TC * wc >= a.M;  // no tokens: the wave only keeps the barriers
+  const bool idle = copies || m0 + 16 * TC * wc >= mend;  // no tokens: the wave only keeps the barriers
   if (copies)
     run_copies();
   else if (idle)
@@ -284,7 +303,7 @@ __global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
   else
     run(std::true_type());
 
-  if (S > 1) {  // unscaled fp32 partials of this K slice, one 16-byte store where it can
+  if (!RG && S > 1) {  // unscaled fp32 partials of this K slice, one 16-byte store where it can
     if (idle) return;
 #pragma unroll
     for (int t = 0; t < RPW; ++t)
@@ -305,7 +324,11 @@ __global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
   }
   const bool via_lds = !a.out_f32 && ((uintptr_t)MD.Y % 16 == 0) && (MD.ldy % 8 == 0) && (rblk % 8 == 0);
   EpiScales<RPW, TC> es;
-  if (!idle) epi_scales(es, MD.sw, a.sx, a.M, rblk + 16 * RPW * wr + 4 * lq, m0 + 16 * TC * wc + li, rowend);
+  const float* sw = RG && MD.sw ? MD.sw + ex * er.N : MD.sw;
+  if (!idle) {
+    epi_scales(es, sw, RG ? nullptr : a.sx, a.M, rblk + 16 * RPW * wr + 4 * lq, m0 + 16 * TC * wc + li, rowend);
+    if constexpr (RG) source_scales<TC>(es.x, er, a.sx, m0 + 16 * TC * wc + li, mend);
+  }
   if (!via_lds) {
     if (idle) return;
 #pragma unroll
@@ -313,15 +336,22 @@ __global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
 #pragma unroll
       for (int c = 0; c < TC; ++c) {
         const int m = m0 + 16 * (TC * wc + c) + li, n0 = rblk + 16 * (RPW * wr + t) + 4 * lq;
-        if (m < a.M && n0 < rowend) store4e(MD.Y, MD.ldy, MD.sw != nullptr, MD.vec_store, a, es, t, c, acc[t][c], m, n0, rowend);
+        if (m < mend && n0 < rowend) store4e(MD.Y, MD.ldy, MD.sw != nullptr, MD.vec_store, a, es, t, c, acc[t][c], m, n0, rowend);
       }
     return;
   }
   barrier_vm_lgkm0<0>();  // every wave's last operand reads and copies are done
   if (!idle) out_tile_write<RPW, TC, kMidRows / 8>(mid_lds, acc, es, MD.sw != nullptr, wr, wc, li, lq);
   barrier_vm_lgkm0<0>();
-  out_tile_store<kMidRows / 8, 768>(mid_lds, kMidTok, m0, a.M, rblk, rowend, MD.Y, MD.ldy);
+  out_tile_store<kMidRows / 8, 768>(mid_lds, kMidTok, m0, mend, rblk, rowend, MD.Y, MD.ldy);
 }
+
+template <int DT>
+__global__ __launch_bounds__(768) void spense_gemm_mid_kernel(GemmArgs a) {
+  mid_body<DT, false>(a, ExpertRows{});
+}
+
+__global__ __launch_bounds__(768) void spense_experts_mid_kernel(GemmArgs a, ExpertRows er) { mid_body<kFP8, true>(a, er); }
 
 }  // namespace
 
@@ -335,6 +365,15 @@ hipError_t launch_mid(int dtype, const GemmArgs& a, hipStream_t s) {
   hipError_t e = set_big_lds(k, 1, dtype == kFP8 ? 0 : 1, kMidLds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k, dim3(a.groups), dim3(768), kMidLds, s, a);
+  return hipGetLastError();
+}
+
+// One launch over the tiles of 128 positions that n rows in er.count groups can have.
+hipError_t launch_experts_mid(const GemmArgs& a, const ExpertRows& er, hipStream_t s) {
+  hipError_t e = set_big_lds(spense_experts_mid_kernel, 1, 2, kMidLds);
+  if (e != hipSuccess) return e;
+  const int64_t grid = most_tiles(er.n, er.count, false, kMidTok) * er.row_blocks;
+  hipLaunchKernelGGL(spense_experts_mid_kernel, dim3((unsigned)grid), dim3(768), kMidLds, s, a, er);
   return hipGetLastError();
 }
 

@@ -101,6 +101,18 @@ __device__ __forceinline__ float glu_silu(float g, float u) {
   return u * (g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)));
 }
 
+// Rows grouped by expert (spense_gemm_experts), beside GemmArgs: positions [0, n) of the
+// grouped rows, the groups' offsets, and where a position's activations are.
+struct ExpertRows {
+  const int32_t* order;  // NULL: position p is activation row p
+  const int32_t* offsets;
+  int32_t n, count;
+  int32_t top;         // activation row = order[p] / top
+  int32_t rows_x;      // activation rows
+  int32_t N;           // rows of an expert's weight: the distance of the experts' scales
+  int32_t row_blocks;  // workgroups of a tile of positions
+};
+
 struct LaunchShape {
   int ct;       // 16-column tiles of M per workgroup (1, 2, 4)
   int rt;       // 16-row tiles per workgroup (1, 2, 4)
@@ -118,6 +130,9 @@ struct LaunchShape {
 hipError_t launch_big2(int dtype, const GemmArgs& a, hipStream_t s);
 // The 128 x 128 kernel (LaunchShape::big == 3): tiled fp8 or row-major bf16 weights.
 hipError_t launch_mid(int dtype, const GemmArgs& a, hipStream_t s);
+
+// Products grouped by expert: the 128 x 128 kernel over tiles of positions, and the row-split one.
+hipError_t launch_experts_mid(const GemmArgs& a, const ExpertRows& er, hipStream_t s);
 
 hipError_t launch_gemm(int dtype, const LaunchShape& ls, const GemmArgs& a, hipStream_t s);
 

@@ -1,7 +1,6 @@
 // Device helper of the kernels that work on rows grouped by an index (spense_group_rows).
 #pragma once
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "spense_internal.h"
 
 namespace spense {
 namespace {
@@ -62,6 +61,24 @@ __device__ __forceinline__ bool find_tile(const int32_t* __restrict__ offsets, i
   out.p0 = __builtin_amdgcn_readlane(p0, src);
   out.p1 = __builtin_amdgcn_readlane(p1, src);
   return true;
+}
+
+// The activation row of position p < n, -1 where order names none.
+__device__ __forceinline__ int source_row(const ExpertRows& er, int p) {
+  if (!er.order) return p < er.rows_x ? p : -1;
+  const int i = er.order[p];
+  const int r = (int)((unsigned)i / (unsigned)er.top);
+  return i >= 0 && r < er.rows_x ? r : -1;
+}
+
+// The token scales of positions p, p + 16, ... below pend (1 elsewhere and without scales).
+template <int CT>
+__device__ __forceinline__ void source_scales(float (&x)[CT], const ExpertRows& er, const float* sx, int p, int pend) {
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int src = sx && p + 16 * c < pend ? source_row(er, p + 16 * c) : -1;
+    x[c] = src >= 0 ? sx[src] : 1.0f;
+  }
 }
 
 // Most tiles that find_tile can give (host).

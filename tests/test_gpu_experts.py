@@ -1,0 +1,308 @@
+"""spense_gemm_experts and mlp_experts through the binding, against the formula in 64 bits.
+
+Integer cases (entries up to 3, power-of-two scales) are exact in every order of summation and
+compared bit for bit.  Random cases: the fp8 matrix instructions add the products of a lane's
+chunk with 13 fractional bits of the largest, so a sum is within (2^-12 + 2 K u) of the sum of
+magnitudes (u = 2^-24), then two scales and half a step of the output type.
+"""
+import sys
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def S():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2606_10445_amd as S
+    return S
+
+
+def say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+def weights(S, g, E, N, K, split, db, ints):
+    """(PackedExperts, E x N x K float64 values, E x N scales)."""
+    draw = torch.randint(-3, 4, (E, N, K), generator=g).float() if ints else torch.randn(E, N, K, generator=g)
+    reg = draw[:, :db] if split == 0 else draw[:, :, :db]
+    if reg.numel():  # keep two random entries of each four
+        r = torch.rand(reg.reshape(E, reg.shape[1], -1, 4).shape, generator=g)
+        keep = torch.zeros_like(r).scatter_(-1, r.argsort(-1)[..., :2], 1.0)
+        reg.copy_((reg.reshape(r.shape) * keep).reshape(reg.shape))
+    q = draw.to(torch.float8_e4m3fn)
+    sc = 2.0 ** torch.randint(-2, 3, (E, N), generator=g) if ints else 0.5 + torch.rand(E, N, generator=g)
+    mask = (q.float() != 0).to(torch.uint8)
+    pws = [S.tile(S.compress(q[e].view(torch.uint8).cuda(), mask[e].cuda(), split, db)) for e in range(E)]
+    return S.stack_experts(pws), q.double(), sc.float()
+
+
+def tokens(g, T, K, ints):
+    x = (torch.randint(-3, 4, (T, K), generator=g).float() if ints else torch.randn(T, K, generator=g)).to(torch.float8_e4m3fn)
+    xs = 2.0 ** torch.randint(-2, 3, (T,), generator=g) if ints else 0.5 + torch.rand(T, generator=g)
+    return x, xs.float()
+
+
+def choices(g, kind, T, top, E):
+    if kind == "even":
+        return torch.randint(-1, E, (T, top), generator=g, dtype=torch.int32)
+    if kind == "skewed":
+        return (torch.rand(T, top, generator=g) ** 4 * (E + 1)).int()
+    return torch.full((T, top), E - 1, dtype=torch.int32)  # one expert has them all
+
+
+def check(y, order, offsets, x, xs, W, sc, top, exact, f32):
+    n = int(offsets[-1])
+    for e in range(W.shape[0]):
+        a, b = int(offsets[e]), int(offsets[e + 1])
+        if a == b:
+            continue
+        src = order[a:b].long() // top
+        acc, mag = x[src].double() @ W[e].t(), x[src].double().abs() @ W[e].abs().t()
+        f = sc[e].double()[None, :] * xs[src].double()[:, None]
+        want, got = acc * f, y[a:b]
+        if exact:
+            want = want.float() if f32 else want.float().bfloat16()
+            assert torch.equal(got, want), f"expert {e}"
+        else:
+            err = (2.0 ** -12 + 2 * W.shape[2] * U) * mag * f.abs() + 4 * U * want.abs()
+            half = U if f32 else 2.0 ** -8
+            assert torch.all((got.double() - want).abs() <= err + half * (want.abs() + err)), f"expert {e}"
+    return n
+
+
+CASES = [  # T, top, E, N, K, split, dense_begin
+    (1, 1, 1, 16, 32, 0, 0), (1, 8, 16, 208, 512, 0, 160), (3, 2, 5, 257, 96, 0, 128), (9, 4, 8, 300, 1056, 1, 512),
+    (40, 2, 4, 130, 2080, 1, 1568), (64, 1, 64, 96, 544, 0, 96), (33, 3, 6, 144, 1024, 1, 0), (50, 6, 7, 400, 640, 0, 400),
+    (150, 2, 5, 256, 512, 0, 192), (400, 2, 9, 272, 992, 1, 736), (513, 1, 3, 389, 1536, 0, 256), (260, 4, 2, 128, 320, 1, 320),
+    (700, 3, 1, 130, 416, 0, 64),
+]
+
+
+@pytest.mark.parametrize("T,top,E,N,K,split,db", CASES)
+@pytest.mark.parametrize("kind", ["even", "skewed", "one"])
+def test_experts_exact(S, T, top, E, N, K, split, db, kind):
+    say(f"[experts] T={T} top={top} E={E} {N}x{K} split={split} db={db} {kind}")
+    g = torch.Generator().manual_seed(T + N + K)
+    (pe, W, sc), (x, xs) = weights(S, g, E, N, K, split, db, True), tokens(g, T, K, True)
+    groups = S.group_rows(choices(g, kind, T, top, E).reshape(-1).cuda(), E)
+    order, offsets = groups.order.cpu(), groups.offsets.cpu()
+    for f32 in (False, True):
+        out = torch.full((T * top, N), 9.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+        y, = S.gemm_experts(x.view(torch.uint8).cuda(), [pe], groups, [sc.cuda()], xs.cuda(), top=top, outs=[out], out_f32=f32)
+        n = check(y.cpu(), order, offsets, x, xs, W, sc, top, True, f32)
+        assert torch.all(y[n:] == 9)  # rows of no expert
+
+
+@pytest.mark.parametrize("T,top,E,N,K,split,db", CASES)
+def test_experts_random(S, T, top, E, N, K, split, db):
+    g = torch.Generator().manual_seed(T + N + K + 1)
+    (pe, W, sc), (x, xs) = weights(S, g, E, N, K, split, db, False), tokens(g, T, K, False)
+    groups = S.group_rows(choices(g, "even", T, top, E).reshape(-1).cuda(), E)
+    order, offsets = groups.order.cpu(), groups.offsets.cpu()
+    for f32 in (False, True):
+        call = lambda: S.gemm_experts(x.cuda().view(torch.uint8), [pe], groups, [sc.cuda()], xs.cuda(), top=top, out_f32=f32)[0]  # noqa: E731,B023
+        y = call()
+        n = check(y.cpu(), order, offsets, x, xs, W, sc, top, False, f32)
+        for _ in range(3):
+            assert torch.equal(call()[:n], y[:n])
+
+
+@pytest.mark.parametrize("T,E,N,K,split,db", [(5, 4, 160, 544, 0, 112), (30, 3, 200, 512, 1, 256), (300, 3, 264, 1024, 0, 128)])
+def test_pair_gathered_and_strided(S, T, E, N, K, split, db):
+    """Two weights in one launch equal two launches; gathered rows; X and Y inside wider buffers; no scales."""
+    g = torch.Generator().manual_seed(T)
+    ws = [weights(S, g, E, N, K, split, db, True) for _ in range(2)]
+    x, xs = tokens(g, T, K, True)
+    groups = S.group_rows(choices(g, "even", T, 1, E).reshape(-1).cuda(), E)
+    n = int(groups.offsets[-1])
+    X, XS = x.view(torch.uint8).cuda(), xs.cuda()
+    both = S.gemm_experts(X, [w[0] for w in ws], groups, [w[2].cuda() for w in ws], XS)
+    for y, (pe, W, sc) in zip(both, ws):
+        one, = S.gemm_experts(X, [pe], groups, [sc.cuda()], XS)
+        assert torch.equal(y[:n], one[:n])
+        wide_x = torch.zeros(T, K + 32, dtype=torch.uint8, device="cuda")
+        wide_x[:n, :K] = X[groups.order[:n].long()]
+        wide_x[n:] = 0x7F
+        xs_p = XS[groups.order.long()]
+        out = torch.full((T, N + 5), 3.0, dtype=torch.bfloat16, device="cuda")
+        S.gemm_experts(wide_x[:, :K], [pe], groups, [sc.cuda()], xs_p, gathered=True, outs=[out[:, :N]])
+        assert torch.equal(out[:n, :N], one[:n]) and torch.all(out[:, N:] == 3) and torch.all(out[n:] == 3)
+        plain, = S.gemm_experts(X, [pe], groups, out_f32=True)
+        ones = torch.ones(E, N), torch.ones(T)
+        check(plain.cpu(), groups.order.cpu(), groups.offsets.cpu(), x, ones[1], W, ones[0], 1, True, True)
+
+
+def test_no_rows(S):
+    g = torch.Generator().manual_seed(1)
+    pe, _, _ = weights(S, g, 3, 64, 128, 0, 32, True)
+    X = torch.zeros(6, 128, dtype=torch.uint8, device="cuda")
+    groups = S.group_rows(torch.full((6,), -1, dtype=torch.int32, device="cuda"), 3)
+    out = torch.full((6, 64), 2.0, dtype=torch.bfloat16, device="cuda")
+    S.gemm_experts(X, [pe], groups, outs=[out])
+    assert torch.all(out == 2)
+    y, = S.gemm_experts(X[:0], [pe], S.group_rows(torch.zeros(0, dtype=torch.int32, device="cuda"), 3))
+    assert y.shape == (0, 64)
+
+
+@pytest.mark.parametrize("T", [20, 400])
+def test_rows_outside_give_zeros(S, T):
+    """order and offsets of another making: rows outside X are zeros, offsets past n are n."""
+    g = torch.Generator().manual_seed(2)
+    pe, W, sc = weights(S, g, 2, 64, 128, 0, 32, True)
+    x, xs = tokens(g, T, 128, True)
+    order = torch.arange(T, dtype=torch.int32)
+    order[3], order[8] = -9, 2 ** 31 - 1
+    groups = S.RowGroups(T, 2, order.cuda(), None, torch.tensor([-7, T // 2, 2 ** 31 - 1], dtype=torch.int32, device="cuda"))
+    y, = S.gemm_experts(x.view(torch.uint8).cuda(), [pe], groups, [sc.cuda()], xs.cuda(), out_f32=True)
+    y = y.cpu()
+    assert torch.all(y[3] == 0) and torch.all(y[8] == 0)
+    order = torch.arange(T)
+    y[3], y[8] = (x[3].double() @ W[0].t() * sc[0] * xs[3]).float(), (x[8].double() @ W[0].t() * sc[0] * xs[8]).float()
+    check(y, order, torch.tensor([0, T // 2, T]), x, xs, W, sc, 1, True, True)
+
+
+def test_non_finite_rows_stay_alone(S):
+    g = torch.Generator().manual_seed(3)
+    for T in (24, 300):
+        pe, W, sc = weights(S, g, 2, 96, 512, 0, 64, True)
+        x, xs = tokens(g, T, 512, True)
+        groups = S.group_rows(choices(g, "even", T, 1, 2).reshape(-1).abs().cuda(), 2)
+        X = x.view(torch.uint8).cuda()
+        clean, = S.gemm_experts(X, [pe], groups, [sc.cuda()], xs.cuda())
+        X[5, 7] = 0x7F
+        y, = S.gemm_experts(X, [pe], groups, [sc.cuda()], xs.cuda())
+        at = int(groups.inverse[5])
+        keep = torch.arange(T, device="cuda") != at
+        assert torch.equal(y[keep], clean[keep]) and torch.any(torch.isnan(y[at]))
+
+
+def decoded_glu(S, G, U):
+    q, s = S.glu_quantize_fp8(G, U)
+    return q.cpu().view(torch.float8_e4m3fn), s.cpu()
+
+
+@pytest.mark.parametrize("T,top,E,H,I,db", [(1, 2, 4, 256, 96, 64), (7, 3, 5, 512, 160, 128), (130, 2, 4, 320, 256, 192),
+                                            (300, 2, 2, 256, 128, 0)])
+def test_mlp_experts(S, T, top, E, H, I, db):
+    """The whole path against its steps in 64 bits; H's codes may sit a step off where h / s is near a
+    midpoint, so the oracle takes the codes that the same G and U give."""
+    g = torch.Generator().manual_seed(T + I)
+    gate, up = weights(S, g, E, I, H, 0, db, False), weights(S, g, E, I, H, 0, db, False)
+    down = weights(S, g, E, H, I, 1, db, False)
+    x, xs = tokens(g, T, H, False)
+    xs = xs / H ** 0.5
+    idx, w = choices(g, "even", T, top, E), torch.rand(T, top, generator=g)
+    idx[0] = -1  # a token without experts
+    X, XS = x.view(torch.uint8).cuda(), xs.cuda()
+    sc = [v[2].cuda() for v in (gate, up, down)]
+    y = S.mlp_experts(X, XS, idx.cuda(), w.cuda(), gate[0], up[0], down[0], *sc)
+    groups = S.group_rows(idx.reshape(-1).cuda(), E)
+    n = int(groups.offsets[-1])
+    G, U_ = S.gemm_experts(X, [gate[0], up[0]], groups, sc[:2], XS, top=top, out_f32=True)
+    hq, hs = decoded_glu(S, G[:n].contiguous(), U_[:n].contiguous())
+    order, off = groups.order.cpu().long(), groups.offsets.cpu()
+    want, mag = torch.zeros(T, H, dtype=torch.float64), torch.zeros(T, H, dtype=torch.float64)
+    for e in range(E):
+        for p in range(int(off[e]), int(off[e + 1])):
+            h = hq[p].double() * hs[p].double()
+            row = (h @ down[1][e].t()) * down[2][e].double() * w.reshape(-1)[order[p]].double()
+            want[order[p] // top] += row
+            mag[order[p] // top] += (h.abs() @ down[1][e].abs().t()) * down[2][e].double() * w.reshape(-1)[order[p]].double()
+    err = (2.0 ** -12 + 2 * I * U) * mag + 8 * U * mag
+    assert torch.all((y.cpu().double() - want).abs() <= err + 2.0 ** -8 * (want.abs() + err))
+    assert torch.all(y[0] == 0)
+
+
+def test_captured_and_on_streams(S):
+    g = torch.Generator().manual_seed(11)
+    T, top, E, H, I = 20, 2, 6, 256, 96
+    gate, up, down = weights(S, g, E, I, H, 0, 64, False), weights(S, g, E, I, H, 0, 64, False), weights(S, g, E, H, I, 1, 64, False)
+    sc = [v[2].cuda() for v in (gate, up, down)]
+    x, xs = tokens(g, T, H, False)
+    X, XS, idx, w = x.view(torch.uint8).cuda(), xs.cuda(), choices(g, "even", T, top, E).cuda(), torch.rand(T, top, generator=g).cuda()
+    call = lambda: S.mlp_experts(X, XS, idx, w, gate[0], up[0], down[0], *sc)  # noqa: E731
+    ref = call()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        outs = []
+        for s in streams:
+            with torch.cuda.stream(s):
+                outs.append(call())
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, ref) for o in outs)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o = call()
+    for seed in (1, 2, 3):
+        g = torch.Generator().manual_seed(seed)
+        x, xs = tokens(g, T, H, False)
+        X.copy_(x.view(torch.uint8)), XS.copy_(xs), idx.copy_(choices(g, "skewed", T, top, E))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, call())
+
+
+def test_norm_adapters_experts_together(S):
+    """A block as a program runs it: norm, a projection with adapters, norm around it, experts."""
+    g = torch.Generator().manual_seed(21)
+    T, top, E, H, I, R = 33, 2, 4, 256, 96, 8
+    x = torch.randn(T, H, generator=g).bfloat16().cuda()
+    w1, w2 = 1 + 0.1 * torch.randn(H, generator=g).cuda(), 1 + 0.1 * torch.randn(H, generator=g).cuda()
+    proj = weights(S, g, 1, H, H, 0, 192, False)
+    pe = proj[0]
+    pw = S.PackedWeight(H, H, S.SPENSE_FP8_E4M3FN, 0, 192, pe.values[0], pe.meta[0], pe.dense[0], S.SPENSE_LAYOUT_TILED)
+    psc = (proj[2][0] / H ** 0.5).cuda()
+    A, B = torch.randn(3, R, H, generator=g).bfloat16(), torch.randn(3, H, R, generator=g).bfloat16()
+    pool = S.AdapterPool(A.cuda(), B.cuda(), torch.full((3,), 0.01, device="cuda"))
+    users = torch.randint(-1, 3, (T,), generator=g, dtype=torch.int32)
+    n1 = S.block_norm(x, weight=w1, normed=True)
+    a = S.gemm_adapters(n1.codes, pw, pool, S.group_rows(users.cuda(), 3), psc, n1.scales, A_x=n1.normed)
+    n2 = S.block_norm(x, a, weight=w2, residual_scale=0.5)
+    gate, up, down = weights(S, g, E, I, H, 0, 64, False), weights(S, g, E, I, H, 0, 64, False), weights(S, g, E, H, I, 1, 64, False)
+    idx, w = choices(g, "even", T, top, E).cuda(), torch.rand(T, top, generator=g).cuda()
+    sc = [v[2].cuda() for v in (gate, up, down)]
+    y = S.mlp_experts(n2.codes, n2.scales, idx, w, gate[0], up[0], down[0], *sc)
+    # the projection and adapters in 64 bits from the norm's outputs (tolerances of the single tests)
+    q = n1.codes.cpu().view(torch.float8_e4m3fn).double() * n1.scales.cpu().double()[:, None]
+    base = q @ (proj[1][0] * psc.cpu().double()[:, None]).t()
+    mag = q.abs() @ (proj[1][0] * psc.cpu().double()[:, None]).abs().t()
+    nx = n1.normed.cpu().double()
+    for t in range(T):
+        if users[t] >= 0:
+            v = nx[t] @ A[users[t]].double().t() * 0.01
+            base[t] += v @ B[users[t]].double().t()
+            mag[t] += (nx[t].abs() @ A[users[t]].double().abs().t() * 0.01) @ B[users[t]].double().abs().t()
+    err = (2.0 ** -12 + 2 * H * U + 2.0 ** -16) * mag
+    assert torch.all((a.cpu().double() - base).abs() <= err + 2.0 ** -8 * (base.abs() + err))
+    r = 0.5 * x.cpu().double() + a.cpu().double()
+    assert torch.all((n2.residual.cpu().double() - r).abs() <= 2.0 ** -8 * r.abs() + 1e-6)
+    assert torch.all(torch.isfinite(y)) and y.shape == (T, H)
+
+
+def test_binding_refuses(S):
+    g = torch.Generator().manual_seed(1)
+    pe, _, sc = weights(S, g, 3, 64, 128, 0, 32, True)
+    other, _, _ = weights(S, g, 3, 64, 128, 0, 48, True)
+    X = torch.zeros(6, 128, dtype=torch.uint8, device="cuda")
+    groups = S.group_rows(torch.zeros(6, dtype=torch.int32, device="cuda"), 3)
+    for kw in (dict(experts=[]), dict(experts=[pe] * 3), dict(X=X[:5]), dict(X=X[:, :96]), dict(X=X.bfloat16()), dict(top=0),
+               dict(top=2), dict(groups=S.group_rows(torch.zeros(6, dtype=torch.int32, device="cuda"), 4)),
+               dict(w_scales=[sc]), dict(w_scales=[sc.cuda()[:2]]), dict(w_scales=[None, None]),
+               dict(x_scale=torch.ones(5, device="cuda")), dict(outs=[torch.zeros(6, 63, dtype=torch.bfloat16, device="cuda")])):
+        with pytest.raises((ValueError, TypeError)):
+            S.gemm_experts(**{"X": X, "experts": [pe], "groups": groups, **kw})
+    with pytest.raises(S.SpenseError):
+        S.gemm_experts(X, [pe, other], groups)
+    with pytest.raises(ValueError):
+        S.stack_experts([])
+    row_major = S.PackedWeight.empty(64, 128, S.SPENSE_FP8_E4M3FN, 0, 32)
+    with pytest.raises(ValueError):
+        S.stack_experts([row_major])
+    with pytest.raises(ValueError):
+        S.mlp_experts(X, torch.ones(6, device="cuda"), torch.zeros(5, 2, dtype=torch.int32, device="cuda"),
+                      torch.zeros(5, 2, device="cuda"), pe, pe, pe)

@@ -93,3 +93,39 @@ def test_adapter_workspace_grows_with_the_batch(S):
                 for R in (8, 16, 40, 64, 72, 128):
                     n = S.spense_adapters_workspace_size(M, pool(S, count=count, K=K, R=R))
                     assert n % (M * R * 4) == 0 and 1 <= n // (M * R * 4) <= min(16, max(1, -(-K // 512)))
+
+
+def test_gemm_experts_refuses(S):
+    import ctypes
+
+    P = ctypes.POINTER(S.spense_packed_t)
+
+    def desc(**kw):
+        d = dict(dtype=1, split=0, N=64, K=128, dense_begin=32, values=A, values_ld=64, meta=A, meta_ld=4, dense=A,
+                 dense_ld=128, layout=1)
+        return S.spense_packed_t(**{**d, **kw})
+
+    def call(descs=None, Y=(2 * A,), ldy=(64,), **kw):
+        descs = [desc()] if descs is None else descs
+        k = max(1, len(descs))
+        parr = (P * k)(*[None if d is None else ctypes.pointer(d) for d in descs])
+        a = dict(X=A, rows_x=8, ldx=128, x_scale=None, order=A, top=1, offsets=A, n=8, count=4, weights=len(descs),
+                 packed_array=parr, w_scales_array=None, Y_array=(ctypes.c_void_p * len(Y))(*Y),
+                 ldy_array=(ctypes.c_int64 * len(ldy))(*ldy), out_flags=0, stream=None)
+        return S.spense_gemm_experts(**{**a, **kw})
+
+    for kw, code in ((dict(X=None), -1), (dict(offsets=None), -1), (dict(rows_x=-1), -1), (dict(n=-1), -1), (dict(n=1 << 31), -1),
+                     (dict(top=0), -1), (dict(count=0), -1), (dict(count=1025), -1), (dict(weights=0), -1), (dict(weights=3), -1),
+                     (dict(packed_array=None), -1), (dict(Y_array=None), -1), (dict(ldy_array=None), -1), (dict(out_flags=2), -1),
+                     (dict(ldx=127), -1), (dict(ldx=136), -2), (dict(X=A + 8), -2), (dict(Y=(None,)), -1), (dict(Y=(A + 1,)), -2),
+                     (dict(ldy=(63,)), -1), (dict(rows_x=1 << 30), -1)):
+        assert call(**kw) == code, kw
+        assert S.spense_last_error()
+    for bad, code in ((dict(layout=0), -1), (dict(dtype=2), -1), (dict(K=96 + 8), -2), (dict(values=None), -1), (dict(dense=A + 8), -2),
+                      (dict(K=0), -1), (dict(dense_begin=65), -1)):
+        assert call([desc(**bad)]) == code, bad
+    assert call([None]) == -1
+    two = dict(Y=(2 * A, 4 * A), ldy=(64, 64))
+    for bad in (dict(N=80), dict(K=160), dict(dense_begin=48), dict(split=1)):
+        assert call([desc(), desc(**bad)], **two) == -1, bad
+    assert call(n=0, X=None) == 0
