@@ -671,6 +671,28 @@ int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float*
                         const spense_packed_t* const* packed, const float* const* w_scales, void* const* Y,
                         const int64_t* ldy, uint32_t out_flags, hipStream_t stream);
 
+/* Device workspace (bytes) of spense_gemm_experts_glu_fp8 for n rows, count experts and N gate / up
+ * rows (0 for sizes that the call refuses). */
+size_t spense_gemm_experts_glu_fp8_workspace_size(int64_t n, int32_t count, int64_t N);
+
+/*
+ * The producer half of a GLU MLP of experts (sec. 3.3.1, Eq. (4)): for every position p of an
+ * expert, g and u as spense_gemm_experts gives them for gate and up in fp32, h = u * g / (1 +
+ * exp(-g)), and h quantised per row as by spense_quantize_fp8: q (n x N e4m3fn codes, ldq bytes) and
+ * scales (n fp32), the input of the experts' down projection.  Where every expert gets many
+ * rows the GLU step runs in the epilogue of gate and up; G and U are then never written.  Rows of
+ * positions from offsets[count] on hold unspecified codes and scales.  gate, up: output-split, one
+ * geometry, else as spense_gemm_experts; ws: at least
+ * spense_gemm_experts_glu_fp8_workspace_size(n, count, N) bytes, 256-byte aligned, scratch
+ * between the two launches.  Asynchronous, allocates nothing.  Errors as spense_gemm_experts,
+ * SPENSE_ERR_ARG for a NULL q or scales or ldq < N, SPENSE_ERR_WS for a missing or small workspace,
+ * SPENSE_ERR_ALIGN for a misaligned one.
+ */
+int spense_gemm_experts_glu_fp8(const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order,
+                                int32_t top, const int32_t* offsets, int64_t n, int32_t count, const spense_packed_t* gate,
+                                const spense_packed_t* up, const float* w_scale_gate, const float* w_scale_up, uint8_t* q,
+                                int64_t ldq, float* scales, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Thread-local description of the last error raised on this thread ("" if none). */
 const char* spense_last_error(void);
 

@@ -50,7 +50,8 @@ EXPORTS = ["spense_abi_version", "spense_set_log", "spense_last_error", "spense_
            "spense_obs_prune_workspace_size", "spense_obs_prune_24", "spense_gemm_grouped", "spense_gemm_glu",
            "spense_gemm_glu_pays", "spense_gemm_glu_fp8_workspace_size", "spense_gemm_glu_fp8", "spense_gemm_planned_workspace_size",
            "spense_gemm_planned", "spense_gemm_noalloc", "spense_block_norm", "spense_group_rows", "spense_combine_rows",
-           "spense_adapters_workspace_size", "spense_add_adapters", "spense_gemm_experts"]
+           "spense_adapters_workspace_size", "spense_add_adapters", "spense_gemm_experts",
+           "spense_gemm_experts_glu_fp8_workspace_size", "spense_gemm_experts_glu_fp8"]
 
 
 class SpenseError(RuntimeError):
@@ -160,6 +161,9 @@ def _load():
         "spense_add_adapters": (ctypes.c_int, [p, i32, i64, i64, p, p, p, P(spense_adapters_t), p, i32, i64, p, i64,
                                                u32, p, sz, p]),
         "spense_gemm_experts": (ctypes.c_int, [p, i64, i64, p, p, i32, p, i64, i32, i32, p, p, p, p, u32, p]),
+        "spense_gemm_experts_glu_fp8_workspace_size": (sz, [i64, i32, i64]),
+        "spense_gemm_experts_glu_fp8": (ctypes.c_int, [p, i64, i64, p, p, i32, p, i64, i32, P(spense_packed_t),
+                                                       P(spense_packed_t), p, p, p, i64, p, p, sz, p]),
         "spense_gemm_planned": (ctypes.c_int, [p, i64, i64, P(spense_packed_t), p, p, p, i64, u32, p, sz,
                                                P(spense_plan_override_t), p]),
     }
@@ -348,6 +352,16 @@ def spense_gemm_experts(X, rows_x, ldx, x_scale, order, top, offsets, n, count, 
                         Y_array, ldy_array, out_flags, stream) -> int:
     return _lib.spense_gemm_experts(X, rows_x, ldx, x_scale, order, top, offsets, n, count, weights, packed_array,
                                     w_scales_array, Y_array, ldy_array, out_flags, stream)
+
+
+def spense_gemm_experts_glu_fp8_workspace_size(n: int, count: int, N: int) -> int:
+    return _lib.spense_gemm_experts_glu_fp8_workspace_size(n, count, N)
+
+
+def spense_gemm_experts_glu_fp8(X, rows_x, ldx, x_scale, order, top, offsets, n, count, gate, up, w_scale_gate, w_scale_up,
+                                q, ldq, scales, ws, ws_bytes, stream) -> int:
+    return _lib.spense_gemm_experts_glu_fp8(X, rows_x, ldx, x_scale, order, top, offsets, n, count, gate, up, w_scale_gate,
+                                            w_scale_up, q, ldq, scales, ws, ws_bytes, stream)
 
 
 # ------------------------------------------------------------------ torch helpers
@@ -1118,6 +1132,26 @@ def stack_experts(pws) -> PackedExperts:
                          torch.stack([p.meta for p in pws]), torch.stack([p.dense for p in pws]))
 
 
+def _check_experts(X, experts, groups, w_scales, x_scale, top, gathered):
+    """Shapes, types and devices of a grouped product's inputs."""
+    e0 = experts[0]
+    _check_x(X, SPENSE_FP8_E4M3FN, e0.K)
+    if top < 1:
+        raise ValueError(f"top = {top}")
+    dev = X.device
+    _on_gpu(dev, groups=groups.order)
+    if X.shape[0] * (1 if gathered else top) != groups.n:
+        raise ValueError(f"X has {X.shape[0]} rows, the groups {groups.n}")
+    for w, s in zip(experts, w_scales):
+        if groups.groups != w.count:
+            raise ValueError(f"groups are over {groups.groups} experts, the weights over {w.count}")
+        _on_gpu(dev, experts=w.dense)
+        if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (w.count, w.N) or not s.is_contiguous()
+                              or s.device != dev):
+            raise ValueError(f"w_scale must be a contiguous fp32 tensor of shape {(w.count, w.N)} on {dev}")
+    _check_scale(x_scale, X.shape[0], dev, "x_scale")
+
+
 def gemm_experts(X: torch.Tensor, experts, groups: RowGroups, w_scales=None, x_scale=None, *, top: int = 1,
                  gathered: bool = False, outs=None, out_f32: bool = False):
     """Y_i[p] = X[row(p)] W_{i,e}^T for every position p of every expert e (spense_gemm_experts), one
@@ -1129,27 +1163,12 @@ def gemm_experts(X: torch.Tensor, experts, groups: RowGroups, w_scales=None, x_s
     k = len(experts)
     if k not in (1, 2):
         raise ValueError("one or two weights")
-    e0 = experts[0]
-    _check_x(X, SPENSE_FP8_E4M3FN, e0.K)
-    if top < 1:
-        raise ValueError(f"top = {top}")
-    n, dev = groups.n, X.device
-    for w in experts:
-        if groups.groups != w.count:
-            raise ValueError(f"groups are over {groups.groups} experts, the weights over {w.count}")
-        _on_gpu(dev, experts=w.dense)
-    if X.shape[0] * (1 if gathered else top) != n:
-        raise ValueError(f"X has {X.shape[0]} rows, the groups {n}")
     if w_scales is None:
         w_scales = [None] * k
     if len(w_scales) != k:
         raise ValueError("one w_scale per weight")
-    for w, s in zip(experts, w_scales):
-        if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (w.count, w.N) or not s.is_contiguous()
-                              or s.device != dev):
-            raise ValueError(f"w_scale must be a contiguous fp32 tensor of shape {(w.count, w.N)} on {dev}")
-    _check_scale(x_scale, X.shape[0], dev, "x_scale")
-    _on_gpu(dev, groups=groups.order)
+    _check_experts(X, experts, groups, w_scales, x_scale, top, gathered)
+    n, dev = groups.n, X.device
     if outs is None:
         outs = [None] * k
     if len(outs) != k:
@@ -1161,14 +1180,34 @@ def gemm_experts(X: torch.Tensor, experts, groups: RowGroups, w_scales=None, x_s
     larr = (ctypes.c_int64 * k)(*[_ld(o) for o in outs])
     with _device(dev):
         _check(spense_gemm_experts(_ptr(X), X.shape[0], _ld16(X), _ptr(x_scale), None if gathered else _ptr(groups.order),
-                                   top, _ptr(groups.offsets), n, e0.count, k, parr, sarr, yarr, larr,
+                                   top, _ptr(groups.offsets), n, experts[0].count, k, parr, sarr, yarr, larr,
                                    SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, _stream(dev)))
     return outs
 
 
+def gemm_experts_glu_fp8(X: torch.Tensor, gate: PackedExperts, up: PackedExperts, groups: RowGroups, gate_scale=None,
+                         up_scale=None, x_scale=None, *, top: int = 1, gathered: bool = False,
+                         workspace: Workspace | None = None):
+    """The producer half of a GLU MLP of experts (spense_gemm_experts_glu_fp8): h = up * silu(gate) of every
+    position, quantised per row.  Returns (codes uint8 n x N, scales fp32 n), the input of the experts'
+    down projection (``gathered``); those of positions in no group are unspecified."""
+    _check_experts(X, [gate, up], groups, [gate_scale, up_scale], x_scale, top, gathered)
+    n, N, dev = groups.n, gate.N, X.device
+    q = torch.empty((n, N), dtype=torch.uint8, device=dev)
+    scales = torch.empty(n, dtype=torch.float32, device=dev)
+    ws = workspace or _CallScratch(dev)
+    with _device(dev):
+        wp, wn = ws.get(spense_gemm_experts_glu_fp8_workspace_size(n, gate.count, N))
+        _check(spense_gemm_experts_glu_fp8(_ptr(X), X.shape[0], _ld16(X), _ptr(x_scale),
+                                           None if gathered else _ptr(groups.order), top, _ptr(groups.offsets), n,
+                                           gate.count, ctypes.byref(gate.desc), ctypes.byref(up.desc), _ptr(gate_scale),
+                                           _ptr(up_scale), _ptr(q), N, _ptr(scales), wp, wn, _stream(dev)))
+    return q, scales
+
+
 def mlp_experts(X: torch.Tensor, x_scale: torch.Tensor, idx: torch.Tensor, weights: torch.Tensor, gate: PackedExperts,
                 up: PackedExperts, down: PackedExperts, gate_scale=None, up_scale=None, down_scale=None, out=None,
-                out_f32: bool = False) -> torch.Tensor:
+                out_f32: bool = False, workspace: Workspace | None = None) -> torch.Tensor:
     """A GLU MLP of experts (``mlp`` of each token's choices, summed): idx T x top int32 names each
     token's experts (outside [0, count): none), weights T x top fp32 what each counts.  The rows are
     grouped by expert, gate and up computed for every position, H = up * silu(gate) quantised per row,
@@ -1179,7 +1218,6 @@ def mlp_experts(X: torch.Tensor, x_scale: torch.Tensor, idx: torch.Tensor, weigh
     if top < 1:
         raise ValueError("at least one expert per token")
     groups = group_rows(idx.reshape(-1), gate.count)
-    G, U = gemm_experts(X, [gate, up], groups, [gate_scale, up_scale], x_scale, top=top, out_f32=True)
-    Hq, sh = glu_quantize_fp8(G, U)
+    Hq, sh = gemm_experts_glu_fp8(X, gate, up, groups, gate_scale, up_scale, x_scale, top=top, workspace=workspace)
     D, = gemm_experts(Hq, [down], groups, [down_scale], sh, gathered=True, out_f32=True)
     return combine_rows(D, groups, weights, top, out=out, out_f32=out_f32)

@@ -147,21 +147,46 @@ namespace {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-}  // namespace
+// Kernels of the grouped products.
+enum Kernel { kRows16, kRows32, kRows64, kMid, kBig };
 
-extern "C" int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order,
-                                   int32_t top, const int32_t* offsets, int64_t n, int32_t count, int32_t weights,
-                                   const spense_packed_t* const* packed, const float* const* w_scales, void* const* Y,
-                                   const int64_t* ldy, uint32_t out_flags, hipStream_t stream) {
+// The kernel for n rows in count groups: by the rows an expert gets on average where they spread
+// evenly (the counts themselves are on the device).
+Kernel choose_kernel(int64_t n, int64_t count) {
+  const int64_t avg = n / (count < n ? count : n);
+  return avg <= 12 ? kRows16 : avg <= 24 ? kRows32 : avg < 48 ? kRows64 : avg < 192 ? kMid : kBig;
+}
+
+// One call's checked arguments.
+struct Call {
+  const uint8_t* X;
+  int64_t ldx, xb;
+  const float* x_scale;
+  spense::ExpertRows er;
+  int64_t N, K, db;
+  bool in_split;
+  int weights;
+  spense::MatDesc mat[2];
+  struct {
+    int64_t row0, rows, kbound;
+    int mat;
+  } reg[4];
+  int nreg;
+  bool out_f32;
+};
+
+// Validates everything but the outputs and fills c (mat[i].Y and what depends on it excepted).
+// c.er.n == 0: nothing to do.
+int check_call(Call& c, const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order, int32_t top,
+               const int32_t* offsets, int64_t n, int32_t count, int32_t weights, const spense_packed_t* const* packed,
+               const float* const* w_scales) {
   if (weights < 1 || weights > 2) return api_fail(SPENSE_ERR_ARG, "weights=%d outside [1, 2]", weights);
   if (count < 1 || count > SPENSE_MAX_GROUPS)
     return api_fail(SPENSE_ERR_ARG, "count=%d outside [1, %d]", count, SPENSE_MAX_GROUPS);
-  if (!packed || !Y || !ldy) return api_fail(SPENSE_ERR_ARG, "NULL array");
+  if (!packed) return api_fail(SPENSE_ERR_ARG, "NULL array");
   if (n < 0 || n > INT32_MAX || rows_x < 0 || rows_x > INT32_MAX)
     return api_fail(SPENSE_ERR_ARG, "bad n=%lld rows_x=%lld", (long long)n, (long long)rows_x);
   if (top < 1) return api_fail(SPENSE_ERR_ARG, "top=%d", top);
-  if (out_flags & ~1u) return api_fail(SPENSE_ERR_ARG, "unknown out_flags 0x%x", out_flags);
-  const int64_t out_es = (out_flags & SPENSE_OUT_F32) ? 4 : 2;
   for (int i = 0; i < weights; ++i) {
     if (!packed[i]) return api_fail(SPENSE_ERR_ARG, "packed[%d] is NULL", i);
     int rc = spense::api_check_packed(packed[i]);
@@ -173,108 +198,192 @@ extern "C" int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, c
       return api_fail(SPENSE_ERR_ARG, "the two weights must have one geometry");
   }
   const spense_packed_t& P = *packed[0];
-  const int64_t N = P.N, K = P.K;
-  if (n == 0 || N == 0) return spense::api_ok();
-  if (K < 1) return api_fail(SPENSE_ERR_ARG, "K=0");
+  memset(&c, 0, sizeof c);
+  c.N = P.N, c.K = P.K, c.db = P.dense_begin, c.in_split = P.split == SPENSE_SPLIT_INPUT, c.weights = weights;
+  if (n == 0 || c.N == 0) return SPENSE_OK;
+  if (c.K < 1) return api_fail(SPENSE_ERR_ARG, "K=0");
   if (!X || !offsets) return api_fail(SPENSE_ERR_ARG, "X or offsets is NULL");
-  if (ldx < K) return api_fail(SPENSE_ERR_ARG, "ldx=%lld < K=%lld", (long long)ldx, (long long)K);
+  if (ldx < c.K) return api_fail(SPENSE_ERR_ARG, "ldx=%lld < K=%lld", (long long)ldx, (long long)c.K);
   if (reinterpret_cast<uintptr_t>(X) % 16 || ldx % 16)
     return api_fail(SPENSE_ERR_ALIGN, "X must be 16-byte aligned with a 16-byte multiple row pitch");
-  for (int i = 0; i < weights; ++i) {
-    if (!Y[i]) return api_fail(SPENSE_ERR_ARG, "Y[%d] is NULL", i);
-    if (ldy[i] < N) return api_fail(SPENSE_ERR_ARG, "ldy[%d] < N", i);
-    if (reinterpret_cast<uintptr_t>(Y[i]) % out_es) return api_fail(SPENSE_ERR_ALIGN, "Y[%d] misaligned", i);
-    if (n * ldy[i] > (int64_t)1 << 40) return api_fail(SPENSE_ERR_ARG, "Y[%d] too large", i);
-  }
   const int64_t lim = (int64_t)1 << 31;
-  const int64_t xb = rows_x > 0 ? (rows_x - 1) * ldx + K : 0;
-  if (xb >= lim) return api_fail(SPENSE_ERR_ARG, "X spans 2 GiB or more");
+  c.X = static_cast<const uint8_t*>(X), c.ldx = ldx, c.xb = rows_x > 0 ? (rows_x - 1) * ldx + c.K : 0, c.x_scale = x_scale;
+  if (c.xb >= lim) return api_fail(SPENSE_ERR_ARG, "X spans 2 GiB or more");
   spense_tiled_layout_t T;
-  int rc = spense_tiled_layout(N, K, P.dtype, P.split, P.dense_begin, &T);
+  int rc = spense_tiled_layout(c.N, c.K, P.dtype, P.split, P.dense_begin, &T);
   if (rc) return rc;
   if ((int64_t)T.values_bytes >= lim || (int64_t)T.meta_bytes >= lim || (int64_t)T.dense_bytes >= lim)
     return api_fail(SPENSE_ERR_ARG, "an expert's weight spans 2 GiB or more");
-  const bool in_split = P.split == SPENSE_SPLIT_INPUT;
-  const int64_t db = P.dense_begin;
   // regions: the dense rows of every weight first (their workgroups carry more bytes), then the 2:4 rows
-  struct {
-    int64_t row0, rows, kbound;
-    int mat;
-  } reg[4];
-  int nreg = 0;
-  for (int kind = 0; kind < (in_split ? 1 : 2); ++kind)
+  for (int kind = 0; kind < (c.in_split ? 1 : 2); ++kind)
     for (int i = 0; i < weights; ++i) {
-      if (in_split)
-        reg[nreg++] = {0, N, db, i};
-      else if (kind == 0 && N > db)
-        reg[nreg++] = {db, N - db, 0, i};
-      else if (kind == 1 && db > 0)
-        reg[nreg++] = {0, db, K, i};
+      if (c.in_split)
+        c.reg[c.nreg++] = {0, c.N, c.db, i};
+      else if (kind == 0 && c.N > c.db)
+        c.reg[c.nreg++] = {c.db, c.N - c.db, 0, i};
+      else if (kind == 1 && c.db > 0)
+        c.reg[c.nreg++] = {0, c.db, c.K, i};
     }
-  spense::MatDesc mat[2];
-  bool vec_rows = in_split || db % 4 == 0;
   for (int i = 0; i < weights; ++i)
-    mat[i] = spense::MatDesc{static_cast<const uint8_t*>(packed[i]->values), packed[i]->meta,
-                             static_cast<const uint8_t*>(packed[i]->dense), (uint32_t)T.values_bytes, (uint32_t)T.meta_bytes,
-                             (uint32_t)T.dense_bytes, Y[i], ldy[i], w_scales ? w_scales[i] : nullptr,
-                             vec_rows && ldy[i] % 4 == 0 && reinterpret_cast<uintptr_t>(Y[i]) % (4 * out_es) == 0};
-  spense::ExpertRows er;
-  memset(&er, 0, sizeof er);
-  er.order = order, er.offsets = offsets, er.n = (int32_t)n, er.count = count, er.top = top, er.rows_x = (int32_t)rows_x;
-  er.N = (int32_t)N;
-  const int64_t avg = n / (count < n ? count : n);
-  hipError_t e;
-  if (avg >= 48) {
-    spense::GemmArgs g;
-    memset(&g, 0, sizeof g);
-    g.X = static_cast<const uint8_t*>(X), g.ldx_b = ldx, g.x_bytes = (uint32_t)xb, g.sx = x_scale;
-    g.M = (int32_t)n, g.N = (int32_t)N, g.out_f32 = (out_flags & SPENSE_OUT_F32) ? 1 : 0;
-    g.tiled = 1, g.tblocks = 1, g.nmat = weights, g.nreg = nreg;
-    for (int i = 0; i < weights; ++i) g.mat[i] = mat[i];
-    int64_t blocks = 0;
-    for (int i = 0; i < nreg; ++i) {
-      spense::Region& R = g.reg[i];
-      R.row0 = (int32_t)reg[i].row0, R.rows = (int32_t)reg[i].rows, R.kbound = (int32_t)reg[i].kbound, R.kend = (int32_t)K;
-      R.dense_row_off = in_split ? 0 : (int32_t)db, R.dense_col_off = in_split ? (int32_t)db : 0;
-      R.ksplit = 1, R.mat = reg[i].mat, R.wg0 = (int32_t)blocks, R.nrb = (int32_t)ceil_div(reg[i].rows, 128);
-      blocks += R.nrb;
-    }
-    g.groups = (int32_t)blocks;
-    er.row_blocks = (int32_t)(ceil_div(blocks, 8) * 8);
-    if (spense::most_tiles(n, count, false, 128) * er.row_blocks > INT32_MAX)
-      return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
-    rc = spense::api_check_device();
-    if (rc) return rc;
-    e = spense::launch_experts_mid(g, er, stream);
-  } else {
-    spense::ExpertArgs a;
-    memset(&a, 0, sizeof a);
-    a.X = static_cast<const uint8_t*>(X), a.ldx_b = ldx, a.x_bytes = (uint32_t)xb, a.sx = x_scale;
-    a.K = (int32_t)K, a.kbound = in_split ? (int32_t)db : 0, a.out_f32 = (out_flags & SPENSE_OUT_F32) ? 1 : 0;
-    a.nreg = nreg;
-    for (int i = 0; i < weights; ++i) a.mat[i] = mat[i];
-    int64_t tiles = 0;
-    for (int i = 0; i < nreg; ++i) {
-      a.reg[i] = {(int32_t)tiles, (int32_t)reg[i].row0, (int32_t)reg[i].rows, reg[i].mat, (int32_t)ceil_div(reg[i].kbound, 512),
-                  (int32_t)ceil_div(K - reg[i].kbound, 512)};
-      tiles += ceil_div(reg[i].rows, 16);
-    }
-    a.tiles = (int32_t)tiles;
-    const int ct = avg <= 12 ? 1 : avg <= 24 ? 2 : 4, wv = ct == 1 ? 4 : 8;
-    a.wgs = (int32_t)ceil_div(tiles, wv);
-    const int64_t grid = spense::most_tiles(n, count, false, 16 * ct) * a.wgs;
-    if (grid > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
-    rc = spense::api_check_device();
-    if (rc) return rc;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * wv), 0, stream, a, er); };
-    if (ct == 1)
-      go(spense::experts_rows_kernel<1, 4>);
-    else if (ct == 2)
-      go(spense::experts_rows_kernel<2, 8>);
-    else
-      go(spense::experts_rows_kernel<4, 8>);
-    e = hipGetLastError();
+    c.mat[i] = spense::MatDesc{static_cast<const uint8_t*>(packed[i]->values), packed[i]->meta,
+                               static_cast<const uint8_t*>(packed[i]->dense), (uint32_t)T.values_bytes,
+                               (uint32_t)T.meta_bytes, (uint32_t)T.dense_bytes, nullptr, 0,
+                               w_scales ? w_scales[i] : nullptr, 0};
+  c.er.order = order, c.er.offsets = offsets, c.er.n = (int32_t)n, c.er.count = count, c.er.top = top;
+  c.er.rows_x = (int32_t)rows_x, c.er.N = (int32_t)c.N;
+  return SPENSE_OK;
+}
+
+void set_output(Call& c, int i, void* Y, int64_t ldy, bool f32) {
+  c.out_f32 = f32;
+  c.mat[i].Y = Y, c.mat[i].ldy = ldy;
+  c.mat[i].vec_store = (c.in_split || c.db % 4 == 0) && ldy % 4 == 0 && reinterpret_cast<uintptr_t>(Y) % (f32 ? 16 : 8) == 0;
+}
+
+// A launch of the 128 x 128 or, with `big`, the 256 x 256 kernel; pmax: the gate / up pair, the
+// fp32 H to mat[0].Y and its row maxima (pmax_ld of them a row) to pmax.
+int launch_tiles(Call& c, bool big, float* pmax, int64_t pmax_ld, hipStream_t stream) {
+  spense::GemmArgs g;
+  memset(&g, 0, sizeof g);
+  g.X = c.X, g.ldx_b = c.ldx, g.x_bytes = (uint32_t)c.xb, g.sx = c.x_scale;
+  g.M = c.er.n, g.N = (int32_t)c.N, g.out_f32 = c.out_f32;
+  g.tiled = 1, g.tblocks = 1, g.nmat = c.weights;
+  g.mat[0] = c.mat[0], g.mat[1] = c.mat[1];
+  g.hmax = pmax, g.hmax_ld = (int32_t)pmax_ld;
+  const int64_t rows = pmax || !big ? 128 : 256;
+  int64_t blocks = 0;
+  for (int i = 0; i < c.nreg; ++i) {
+    if (pmax && c.reg[i].mat) continue;  // a pair's regions are the gate's
+    spense::Region& R = g.reg[g.nreg++];
+    R.row0 = (int32_t)c.reg[i].row0, R.rows = (int32_t)c.reg[i].rows;
+    R.kbound = (int32_t)c.reg[i].kbound, R.kend = (int32_t)c.K;
+    R.dense_row_off = c.in_split ? 0 : (int32_t)c.db, R.dense_col_off = c.in_split ? (int32_t)c.db : 0;
+    R.ksplit = 1, R.mat = c.reg[i].mat, R.wg0 = (int32_t)blocks, R.nrb = (int32_t)ceil_div(c.reg[i].rows, rows);
+    blocks += R.nrb;
   }
-  if (e != hipSuccess) return api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));
+  g.groups = (int32_t)blocks, g.hg0 = g.groups;
+  c.er.row_blocks = (int32_t)(ceil_div(blocks, 8) * 8);
+  if (spense::most_tiles(c.er.n, c.er.count, false, big ? 256 : 128) * c.er.row_blocks > INT32_MAX)
+    return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
+  int rc = spense::api_check_device();
+  if (rc) return rc;
+  const hipError_t e = big ? spense::launch_experts_big2(g, c.er, stream) : spense::launch_experts_mid(g, c.er, stream);
+  return e == hipSuccess ? SPENSE_OK : api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));
+}
+
+int launch_rows(Call& c, int ct, hipStream_t stream) {
+  spense::ExpertArgs a;
+  memset(&a, 0, sizeof a);
+  a.X = c.X, a.ldx_b = c.ldx, a.x_bytes = (uint32_t)c.xb, a.sx = c.x_scale;
+  a.K = (int32_t)c.K, a.kbound = c.in_split ? (int32_t)c.db : 0, a.out_f32 = c.out_f32, a.nreg = c.nreg;
+  a.mat[0] = c.mat[0], a.mat[1] = c.mat[1];
+  int64_t tiles = 0;
+  for (int i = 0; i < c.nreg; ++i) {
+    a.reg[i] = {(int32_t)tiles, (int32_t)c.reg[i].row0, (int32_t)c.reg[i].rows, c.reg[i].mat,
+                (int32_t)ceil_div(c.reg[i].kbound, 512), (int32_t)ceil_div(c.K - c.reg[i].kbound, 512)};
+    tiles += ceil_div(c.reg[i].rows, 16);
+  }
+  a.tiles = (int32_t)tiles;
+  const int wv = ct == 1 ? 4 : 8;
+  a.wgs = (int32_t)ceil_div(tiles, wv);
+  const int64_t grid = spense::most_tiles(c.er.n, c.er.count, false, 16 * ct) * a.wgs;
+  if (grid > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
+  int rc = spense::api_check_device();
+  if (rc) return rc;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * wv), 0, stream, a, c.er); };
+  if (ct == 1)
+    go(spense::experts_rows_kernel<1, 4>);
+  else if (ct == 2)
+    go(spense::experts_rows_kernel<2, 8>);
+  else
+    go(spense::experts_rows_kernel<4, 8>);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SPENSE_OK : api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));
+}
+
+int launch_products(Call& c, hipStream_t stream) {
+  const Kernel k = choose_kernel(c.er.n, c.er.count);
+  if (k >= kMid) return launch_tiles(c, k == kBig, nullptr, 0, stream);
+  return launch_rows(c, k == kRows16 ? 1 : k == kRows32 ? 2 : 4, stream);
+}
+
+// The workspace of the gate / up pair: H, or G then U, fp32 with rows padded to 64 elements, and
+// behind H its row maxima (two per block of 128 weight rows and region).
+int64_t glu_ld(int64_t N) { return ceil_div(N, 64) * 64; }
+int64_t glu_maxima(int64_t N) { return 2 * (ceil_div(N, 128) + 1); }
+int64_t glu_rows_bytes(int64_t n, int64_t N) { return ceil_div(n * glu_ld(N) * 4, 256) * 256; }
+
+}  // namespace
+
+extern "C" {
+
+int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order, int32_t top,
+                        const int32_t* offsets, int64_t n, int32_t count, int32_t weights,
+                        const spense_packed_t* const* packed, const float* const* w_scales, void* const* Y,
+                        const int64_t* ldy, uint32_t out_flags, hipStream_t stream) {
+  Call c;
+  int rc = check_call(c, X, rows_x, ldx, x_scale, order, top, offsets, n, count, weights, packed, w_scales);
+  if (rc) return rc;
+  if (!Y || !ldy) return api_fail(SPENSE_ERR_ARG, "NULL array");
+  if (out_flags & ~1u) return api_fail(SPENSE_ERR_ARG, "unknown out_flags 0x%x", out_flags);
+  if (c.er.n == 0) return spense::api_ok();
+  const bool f32 = (out_flags & SPENSE_OUT_F32) != 0;
+  for (int i = 0; i < weights; ++i) {
+    if (!Y[i]) return api_fail(SPENSE_ERR_ARG, "Y[%d] is NULL", i);
+    if (ldy[i] < c.N) return api_fail(SPENSE_ERR_ARG, "ldy[%d] < N", i);
+    if (reinterpret_cast<uintptr_t>(Y[i]) % (f32 ? 4 : 2)) return api_fail(SPENSE_ERR_ALIGN, "Y[%d] misaligned", i);
+    if (n * ldy[i] > (int64_t)1 << 40) return api_fail(SPENSE_ERR_ARG, "Y[%d] too large", i);
+    set_output(c, i, Y[i], ldy[i], f32);
+  }
+  rc = launch_products(c, stream);
+  return rc ? rc : spense::api_ok();
+}
+
+size_t spense_gemm_experts_glu_fp8_workspace_size(int64_t n, int32_t count, int64_t N) {
+  if (n < 1 || n > INT32_MAX || N < 1 || N > INT32_MAX || count < 1 || count > SPENSE_MAX_GROUPS) return 0;
+  if (choose_kernel(n, count) == kBig) return (size_t)(glu_rows_bytes(n, N) + n * glu_maxima(N) * 4);
+  return (size_t)(2 * glu_rows_bytes(n, N));
+}
+
+int spense_gemm_experts_glu_fp8(const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order,
+                                int32_t top, const int32_t* offsets, int64_t n, int32_t count, const spense_packed_t* gate,
+                                const spense_packed_t* up, const float* w_scale_gate, const float* w_scale_up, uint8_t* q,
+                                int64_t ldq, float* scales, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const spense_packed_t* const packed[2] = {gate, up};
+  const float* const w_scales[2] = {w_scale_gate, w_scale_up};
+  Call c;
+  int rc = check_call(c, X, rows_x, ldx, x_scale, order, top, offsets, n, count, 2, packed, w_scales);
+  if (rc) return rc;
+  if (c.er.n == 0) return spense::api_ok();
+  if (c.in_split) return api_fail(SPENSE_ERR_ARG, "gate and up must be output-split");
+  if (!q || !scales) return api_fail(SPENSE_ERR_ARG, "q or scales is NULL");
+  if (ldq < c.N) return api_fail(SPENSE_ERR_ARG, "ldq=%lld < N=%lld", (long long)ldq, (long long)c.N);
+  const size_t need = spense_gemm_experts_glu_fp8_workspace_size(n, count, c.N);
+  if (!ws || ws_bytes < need)
+    return api_fail(SPENSE_ERR_WS, "workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
+  if (reinterpret_cast<uintptr_t>(ws) % 256) return api_fail(SPENSE_ERR_ALIGN, "workspace must be 256-byte aligned");
+  if (n * ceil_div(c.N, 2048) > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "n x N too large for the quantisation grid");
+  const int64_t ld = glu_ld(c.N), half = glu_rows_bytes(n, c.N);
+  float* const H = static_cast<float*>(ws);
+  float* const second = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + half);
+  hipError_t e;
+  if (choose_kernel(n, count) == kBig) {
+    int64_t blocks = 0;
+    for (int i = 0; i < c.nreg; ++i)
+      if (c.reg[i].mat == 0) blocks += ceil_div(c.reg[i].rows, 128);
+    set_output(c, 0, H, ld, true);
+    rc = launch_tiles(c, true, second, 2 * blocks, stream);
+    if (rc) return rc;
+    e = spense::launch_quantize_rowmax(H, ld, n, c.N, second, (int)(2 * blocks), q, ldq, scales, stream);
+  } else {
+    set_output(c, 0, H, ld, true);
+    set_output(c, 1, second, ld, true);
+    rc = launch_products(c, stream);
+    if (rc) return rc;
+    e = spense::launch_glu_quantize(SPENSE_F32, H, ld * 4, second, ld * 4, n, c.N, q, ldq, scales, stream);
+  }
+  if (e != hipSuccess) return api_fail(SPENSE_ERR_HIP, "experts quantise launch failed: %s", hipGetErrorString(e));
   return spense::api_ok();
 }
+
+}  // extern "C"

@@ -1,5 +1,6 @@
 // The 256 x 256 large-M kernel (spense_gemm.hip has the overview of all GEMM kernels).
 #include "spense_gemm_device.h"
+#include "spense_rows_device.h"
 
 namespace spense {
 namespace {
@@ -67,8 +68,9 @@ __device__ __forceinline__ void keep_scalar(T& v) {
 
 enum { kB2Plain = 0, kB2Grouped = 1, kB2Glu = 2 };
 
-template <int DT, int MODE>
-__global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
+// RG: rows grouped by expert, as in mid_body, tiles of up to 256 positions.
+template <int DT, int MODE, bool RG>
+__device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& er) {
   constexpr bool TL = DT == kFP8;  // tiled weights; bf16 reads the row-major layout
   constexpr int ES = Traits<DT>::ES;
   typedef std::integral_constant<int, DT> Dt;
@@ -87,7 +89,17 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
   // hrb0 .. of the last region as 256 x 128 tiles, hper per row block.
   int g = blockIdx.x, ri, rb, m0;
   bool half = false;
-  if (g < a.hg0) {
+  RowTile rt = {0, 0, 0};
+  if constexpr (RG) {
+    const int per = er.row_blocks >> 3, x = g & 7, l = g >> 3;
+    g = (l % per) * 8 + x;
+    if (g >= a.groups || !find_tile(er.offsets, er.count, er.n, false, kB2Tokens, l / per, rt)) return;
+    ri = 0;
+    for (int i = 1; i < a.nreg; ++i)
+      if (g >= a.reg[i].wg0) ri = i;
+    rb = g - a.reg[ri].wg0;
+    m0 = rt.p0;
+  } else if (g < a.hg0) {
     if (a.xgt > 0 && g < a.xg1) {  // XCD-aware order, as in spense_gemm_big_kernel
       const int T = a.tblocks, GT = a.xgt, RC = a.xrc, TGc = T / GT;
       const int x = g & 7, l = g >> 3, tg = x % TGc, rc = x / TGc;
@@ -114,7 +126,8 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
   const int rblk = R.row0 + rb * kRows;
   // tokens of this tile: 256, or 192 (full tiles of a 192-token block), or 128 (half tiles), and
   // those that M ends before; its four waves a row half take 16 NT of them each
-  const int ntok = min(half ? kB2Tokens / 2 : (a.btok > 0 ? a.btok : kB2Tokens), a.M - m0);
+  const int mend = RG ? rt.p1 : a.M;
+  const int ntok = RG ? mend - m0 : min(half ? kB2Tokens / 2 : (a.btok > 0 ? a.btok : kB2Tokens), a.M - m0);
   const int K = R.kend * ES, kbound = R.kbound * ES;  // bytes of an activation row
   uint32_t ldx = (uint32_t)a.ldx_b;  // X spans less than 2 GiB
   keep_scalar(ldx);
@@ -127,10 +140,12 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
   // 4 wave .. 4 wave + 3, dense 4 w4 .. 4 w4 + 3)
   const MatDesc& MV = GL ? a.mat[(wave >> 1) & 1] : MD;
   const MatDesc& MM = GL ? a.mat[wave & 1] : MD;
+  const int64_t ex = RG ? rt.group : 0;
   const __amdgpu_buffer_rsrc_t rx = rsrc(a.X, a.x_bytes),
-                               rv = GR || GL ? rsrc(MV.values, MV.v_bytes) : rsrc(a.values, a.v_bytes),
-                               rm = GR || GL ? rsrc(MM.meta, MM.m_bytes) : rsrc(a.meta, a.m_bytes),
-                               rd = GR || GL ? rsrc(MM.dense, MM.d_bytes) : rsrc(a.dense, a.d_bytes);
+                               rv = GR || GL ? rsrc(MV.values + ex * MV.v_bytes, MV.v_bytes) : rsrc(a.values, a.v_bytes),
+                               rm = GR || GL ? rsrc(reinterpret_cast<const uint8_t*>(MM.meta) + ex * MM.m_bytes, MM.m_bytes)
+                                             : rsrc(a.meta, a.m_bytes),
+                               rd = GR || GL ? rsrc(MM.dense + ex * MM.d_bytes, MM.d_bytes) : rsrc(a.dense, a.d_bytes);
   const int n_sp = (kbound + 127) / 128, n_de = (K - kbound + 127) / 128;
   const int nch_sp = (n_sp + 3) / 4, nch_de = (n_de + 3) / 4;
 
@@ -165,7 +180,12 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = 32 * wave + 8 * i + (lane >> 3), m = m0 + r;
-      xo[i] = m < a.M && r < ntok ? (uint32_t)m * ldx + (xb ^ (64 * (i & 1))) : kOOB;
+      if constexpr (RG) {
+        const int src = r < ntok ? source_row(er, m) : -1;
+        xo[i] = src >= 0 ? (uint32_t)src * ldx + (xb ^ (64 * (i & 1))) : kOOB;
+      } else {
+        xo[i] = m < a.M && r < ntok ? (uint32_t)m * ldx + (xb ^ (64 * (i & 1))) : kOOB;
+      }
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -297,7 +317,12 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
                      : (uint32_t)((r0 - dense_row_off) * a.d_ld_b + (kbound - R.dense_col_off * ES) + (xb ^ (64 * (i & 1))));
       } else {
         const int r = 64 * w4 + 8 * i + (lane >> 3), m = m0 + r;
-        lo[i] = m < a.M && r < ntok ? (uint32_t)m * ldx + kbound + (xb ^ (64 * (i & 1))) : kOOB;
+        if constexpr (RG) {
+          const int src = r < ntok ? source_row(er, m) : -1;
+          lo[i] = src >= 0 ? (uint32_t)src * ldx + kbound + (xb ^ (64 * (i & 1))) : kOOB;
+        } else {
+          lo[i] = m < a.M && r < ntok ? (uint32_t)m * ldx + kbound + (xb ^ (64 * (i & 1))) : kOOB;
+        }
       }
     }
     auto x_copy = [&](int s) __attribute__((always_inline)) {
@@ -386,13 +411,14 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
   const bool via_lds = !GL && !a.out_f32 && ((uintptr_t)MD.Y % 16 == 0) && (MD.ldy % 8 == 0) && (rblk % 8 == 0);
   const int mw = m0 + 16 * NT * wc + li;
   if constexpr (GL) {
-    const float* const sg = a.mat[0].sw;
-    const float* const su = a.mat[1].sw;
+    const float* const sg = RG && a.mat[0].sw ? a.mat[0].sw + ex * er.N : a.mat[0].sw;
+    const float* const su = RG && a.mat[1].sw ? a.mat[1].sw + ex * er.N : a.mat[1].sw;
     const int nw = rblk + 64 * wr + 4 * lq;
     EpiScales<RPW / 2, NT> eg;
     EpiScales<RPW / 2, 1> eu;
-    epi_scales(eg, sg, a.sx, a.M, nw, mw, rowend);
+    epi_scales(eg, sg, RG ? nullptr : a.sx, a.M, nw, mw, rowend);
     epi_scales(eu, su, nullptr, a.M, nw, mw, rowend);
+    if constexpr (RG) source_scales<NT>(eg.x, er, a.sx, mw, mend);
     // the row block's number over both regions: its two slots of the row maxima
     const int slot = 2 * (R.wg0 / a.tblocks + rb) + wr;
 #pragma unroll
@@ -411,18 +437,20 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
           h[r] = glu_silu(gg * eg.x[c], uu * eg.x[c]);
           if (n0 + r < rowend) tmax = fmaxf(tmax, fabsf(h[r]));
         }
-        if (m < a.M && n0 < rowend) put4(MD.Y, MD.ldy, MD.vec_store, a, h, m, n0, rowend);
+        if (m < mend && n0 < rowend) put4(MD.Y, MD.ldy, MD.vec_store, a, h, m, n0, rowend);
       }
       if (a.hmax) {
         tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
         tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
-        if (lq == 0 && m < a.M) a.hmax[(int64_t)m * a.hmax_ld + slot] = tmax;
+        if (lq == 0 && m < mend) a.hmax[(int64_t)m * a.hmax_ld + slot] = tmax;
       }
     }
     return;
   }
   EpiScales<RPW, NT> es;
-  epi_scales(es, MD.sw, a.sx, a.M, rblk + 16 * RPW * wr + 4 * lq, mw, rowend);
+  const float* const sw_n = RG && MD.sw ? MD.sw + ex * er.N : MD.sw;
+  epi_scales(es, sw_n, RG ? nullptr : a.sx, a.M, rblk + 16 * RPW * wr + 4 * lq, mw, rowend);
+  if constexpr (RG) source_scales<NT>(es.x, er, a.sx, mw, mend);
   if (!via_lds) {
     void* Y = MD.Y;
     int64_t ldy = MD.ldy;
@@ -436,14 +464,14 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
       for (int c = 0; c < NT; ++c) {
         const int m = mw + 16 * c;
         const int n0 = rblk + 16 * (RPW * wr + t) + 4 * lq;
-        if (m < a.M && n0 < rowend) store4e(Y, ldy, MD.sw != nullptr, vec_store, a, es, t, c, acc[t][c], m, n0, rowend);
+        if (m < mend && n0 < rowend) store4e(Y, ldy, MD.sw != nullptr, vec_store, a, es, t, c, acc[t][c], m, n0, rowend);
       }
     return;
   }
   barrier_vm_lgkm0<0>();  // every wave's last operand reads and copies are done
   out_tile_write<RPW, NT, kB2Rows / 8>(big_lds, acc, es, MD.sw != nullptr, wr, wc, li, lq);
   barrier_vm_lgkm0<0>();
-  out_tile_store<kB2Rows / 8, 512>(big_lds, ntok, m0, a.M, rblk, rowend, MD.Y, MD.ldy);
+  out_tile_store<kB2Rows / 8, 512>(big_lds, ntok, m0, mend, rblk, rowend, MD.Y, MD.ldy);
   };
   if (ntok > 192)
     tile(std::integral_constant<int, 4>());
@@ -451,6 +479,16 @@ __global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
     tile(std::integral_constant<int, 3>());
   else
     tile(std::integral_constant<int, 2>());
+}
+
+template <int DT, int MODE>
+__global__ __launch_bounds__(512) void spense_gemm_big2_kernel(GemmArgs a) {
+  big2_body<DT, MODE, false>(a, ExpertRows{});
+}
+
+template <int MODE>
+__global__ __launch_bounds__(512) void spense_experts_big2_kernel(GemmArgs a, ExpertRows er) {
+  big2_body<kFP8, MODE, true>(a, er);
 }
 
 }  // namespace
@@ -468,6 +506,18 @@ hipError_t launch_big2(int dtype, const GemmArgs& a, hipStream_t s) {
   hipError_t e = set_big_lds(k, a.tiled ? 1 : 0, 2 + mode, kB2Lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k, dim3(a.groups), dim3(512), kB2Lds, s, a);
+  return hipGetLastError();
+}
+
+// One launch over the tiles of 256 positions that n rows in er.count groups can have; with hmax_ld,
+// the gate / up pair.
+hipError_t launch_experts_big2(const GemmArgs& a, const ExpertRows& er, hipStream_t s) {
+  const bool glu = a.hmax_ld > 0;
+  auto k = glu ? spense_experts_big2_kernel<kB2Glu> : spense_experts_big2_kernel<kB2Grouped>;
+  hipError_t e = set_big_lds(k, 0, glu ? 1 : 0, kB2Lds);
+  if (e != hipSuccess) return e;
+  const int64_t grid = most_tiles(er.n, er.count, false, kB2Tokens) * er.row_blocks;
+  hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(512), kB2Lds, s, a, er);
   return hipGetLastError();
 }
 

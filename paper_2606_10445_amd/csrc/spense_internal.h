@@ -131,8 +131,9 @@ hipError_t launch_big2(int dtype, const GemmArgs& a, hipStream_t s);
 // The 128 x 128 kernel (LaunchShape::big == 3): tiled fp8 or row-major bf16 weights.
 hipError_t launch_mid(int dtype, const GemmArgs& a, hipStream_t s);
 
-// Products grouped by expert: the 128 x 128 kernel over tiles of positions, and the row-split one.
+// Products grouped by expert: the 128 x 128 and the 256 x 256 kernel over tiles of positions.
 hipError_t launch_experts_mid(const GemmArgs& a, const ExpertRows& er, hipStream_t s);
+hipError_t launch_experts_big2(const GemmArgs& a, const ExpertRows& er, hipStream_t s);
 
 hipError_t launch_gemm(int dtype, const LaunchShape& ls, const GemmArgs& a, hipStream_t s);
 

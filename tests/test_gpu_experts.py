@@ -97,6 +97,43 @@ def test_experts_exact(S, T, top, E, N, K, split, db, kind):
         assert torch.all(y[n:] == 9)  # rows of no expert
 
 
+LARGE = [  # many rows an expert: tiles of up to 256 positions, of every number of 64-token quarters
+    (450, 1, 2, 300, 352, 0, 112), (700, 2, 3, 513, 544, 1, 288), (1100, 1, 4, 272, 640, 0, 0), (520, 2, 2, 136, 256, 0, 136),
+    (999, 3, 5, 264, 480, 1, 0), (640, 1, 1, 400, 1056, 1, 1056),
+]
+
+
+@pytest.mark.parametrize("T,top,E,N,K,split,db", LARGE)
+@pytest.mark.parametrize("kind", ["even", "skewed", "one"])
+def test_large_groups_exact(S, T, top, E, N, K, split, db, kind):
+    test_experts_exact(S, T, top, E, N, K, split, db, kind)
+
+
+@pytest.mark.parametrize("T,top,E,N,K,split,db", LARGE)
+def test_large_groups_random(S, T, top, E, N, K, split, db):
+    test_experts_random(S, T, top, E, N, K, split, db)
+
+
+@pytest.mark.parametrize("T,top,E,N,K,db", [(1, 4, 8, 96, 256, 64), (40, 2, 5, 130, 512, 96), (90, 2, 4, 160, 320, 160),
+                                            (150, 3, 6, 257, 544, 128), (600, 1, 2, 300, 352, 112), (900, 2, 3, 513, 512, 0),
+                                            (700, 2, 4, 136, 416, 136)])
+@pytest.mark.parametrize("kind", ["even", "skewed"])
+def test_glu_pair(S, T, top, E, N, K, db, kind):
+    """The producer half of the MLP gives the codes and scales of its steps, bit for bit."""
+    say(f"[glu] T={T} top={top} E={E} {N}x{K} db={db} {kind}")
+    g = torch.Generator().manual_seed(T + N)
+    gate, up = weights(S, g, E, N, K, 0, db, False), weights(S, g, E, N, K, 0, db, False)
+    x, xs = tokens(g, T, K, False)
+    X, XS, sc = x.view(torch.uint8).cuda(), xs.cuda() / K ** 0.5, [gate[2].cuda(), up[2].cuda()]
+    groups = S.group_rows(choices(g, kind, T, top, E).reshape(-1).cuda(), E)
+    n = int(groups.offsets[-1])
+    for scales in ((sc, XS), ([None, None], None)):
+        G, U_ = S.gemm_experts(X, [gate[0], up[0]], groups, *scales, top=top, out_f32=True)
+        want = S.glu_quantize_fp8(G[:n].contiguous(), U_[:n].contiguous())
+        q, s = S.gemm_experts_glu_fp8(X, gate[0], up[0], groups, *scales[0], scales[1], top=top)
+        assert torch.equal(s[:n], want[1]) and torch.equal(q[:n], want[0])
+
+
 @pytest.mark.parametrize("T,top,E,N,K,split,db", CASES)
 def test_experts_random(S, T, top, E, N, K, split, db):
     g = torch.Generator().manual_seed(T + N + K + 1)
