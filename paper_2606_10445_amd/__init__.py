@@ -377,7 +377,13 @@ def _storage_dtype(dtype: int):
     return torch.uint8 if dtype == SPENSE_FP8_E4M3FN else torch.int16
 
 
+# the current stream's handle without making a torch.cuda.Stream (1.8 us of host time a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(device) -> int:
+    if _raw_stream is not None and device.index is not None:
+        return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
 
 
@@ -888,12 +894,13 @@ def _device(dev):
     return _here if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
 
 
-def _on_gpu(dev, **tensors):
+def _on_gpu(dev, *tensors):
+    """All of these tensors (None: absent) are on the GPU ``dev``."""
     if dev.type != "cuda":
         raise ValueError(f"tensors must be on a GPU, not on {dev}")
-    for name, t in tensors.items():
+    for t in tensors:
         if t is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, expected {dev}")
+            raise ValueError(f"a tensor of shape {tuple(t.shape)} is on {t.device}, expected {dev}")
 
 
 def _rows_of(t, name, shape, dtype=None):
@@ -963,20 +970,23 @@ def block_norm(x: torch.Tensor, y: torch.Tensor | None = None, *, post_weight=No
     quantize = quantize or codes_out is not None or scales_out is not None
     if y is None and residual_out is not None:
         raise ValueError("without y there is no new residual")
-    _on_gpu(dev, y=y, gate=gate, post_weight=post_weight, weight=weight, residual_out=residual_out,
-            normed_out=normed_out, codes_out=codes_out, scales_out=scales_out)
+    _on_gpu(dev, y, gate, post_weight, weight, residual_out, normed_out, codes_out, scales_out)
     r = n = q = s = None
     if y is not None:
+        if residual_out is not None:
+            _rows_of(residual_out, "residual_out", (M, K), x.dtype)
         r = torch.empty((M, K), dtype=x.dtype, device=dev) if residual_out is None else residual_out
-        _rows_of(r, "residual_out", (M, K), x.dtype)
     if normed:
+        if normed_out is not None:
+            _rows_of(normed_out, "normed_out", (M, K), ydtype)
         n = torch.empty((M, K), dtype=ydtype, device=dev) if normed_out is None else normed_out
-        _rows_of(n, "normed_out", (M, K), ydtype)
     if quantize:
+        if codes_out is not None:
+            _rows_of(codes_out, "codes_out", (M, K), torch.uint8)
+        if scales_out is not None:
+            _check_scale(scales_out, M, dev, "scales_out")
         q = torch.empty((M, K), dtype=torch.uint8, device=dev) if codes_out is None else codes_out
         s = torch.empty(M, dtype=torch.float32, device=dev) if scales_out is None else scales_out
-        _rows_of(q, "codes_out", (M, K), torch.uint8)
-        _check_scale(s, M, dev, "scales_out")
     if r is None and n is None and q is None:
         raise ValueError("no output is asked for")
     a = spense_block_norm_t(M, K, _ptr(x), _ld(x), xt, yt, _ptr(y), 0 if y is None else _ld(y), _ptr(gate), ldg,
@@ -993,11 +1003,29 @@ class RowGroups:
     """n rows grouped by an index (spense_group_rows), for any number of calls on the same rows:
     ``order`` (n int32, the rows of group 0, 1, ... and then those of no group), ``offsets``
     (groups + 1 int32, group g owns positions [offsets[g], offsets[g + 1])) and ``inverse`` (n int32,
-    each row's position, -1 where it is in no group), all on the device."""
+    each row's position, -1 where it is in no group), all on the device: parts of one buffer."""
 
-    def __init__(self, n, groups, order, inverse, offsets):
-        self.n, self.groups = n, groups
-        self.order, self.inverse, self.offsets = order, inverse, offsets
+    def __init__(self, n, groups, buf):
+        self.n, self.groups, self.buf, self.device = n, groups, buf, buf.device
+        p = buf.data_ptr()
+        self.order_ptr, self.inverse_ptr, self.offsets_ptr = p, p + 4 * n, p + 8 * n
+
+    @property
+    def order(self):
+        return self.buf[:self.n]
+
+    @property
+    def inverse(self):
+        return self.buf[self.n:2 * self.n]
+
+    @property
+    def offsets(self):
+        return self.buf[2 * self.n:]
+
+
+def _same_device(groups, dev):
+    if groups.device != dev:
+        raise ValueError(f"the groups are on {groups.device}, expected {dev}")
 
 
 def group_rows(idx: torch.Tensor, groups: int) -> RowGroups:
@@ -1007,11 +1035,10 @@ def group_rows(idx: torch.Tensor, groups: int) -> RowGroups:
     dev = idx.device
     _on_gpu(dev)
     n = idx.numel()
-    buf = torch.empty(2 * n + max(groups, 0) + 1, dtype=torch.int32, device=dev)
-    order, inverse, offsets = buf[:n], buf[n:2 * n], buf[2 * n:]
+    g = RowGroups(n, groups, torch.empty(2 * n + max(groups, 0) + 1, dtype=torch.int32, device=dev))
     with _device(dev):
-        _check(spense_group_rows(_ptr(idx), n, groups, _ptr(order), _ptr(inverse), _ptr(offsets), _stream(dev)))
-    return RowGroups(n, groups, order, inverse, offsets)
+        _check(spense_group_rows(_ptr(idx), n, groups, g.order_ptr, g.inverse_ptr, g.offsets_ptr, _stream(dev)))
+    return g
 
 
 def combine_rows(D: torch.Tensor, groups: RowGroups, weights: torch.Tensor | None = None, top: int = 1, out=None,
@@ -1025,12 +1052,13 @@ def combine_rows(D: torch.Tensor, groups: RowGroups, weights: torch.Tensor | Non
         raise ValueError(f"D has {n} rows, the groups {groups.n}; both must be T * top with top = {top}")
     T = n // top
     dev = D.device
-    _on_gpu(dev, groups=groups.order, weights=weights)
+    _on_gpu(dev, weights)
+    _same_device(groups, dev)
     if weights is not None and (weights.dtype != torch.float32 or weights.numel() != n or not weights.is_contiguous()):
         raise ValueError(f"weights must be a contiguous fp32 tensor of {n} entries")
     out = _out(out, T, N, out_f32, dev)
     with _device(dev):
-        _check(spense_combine_rows(_ptr(D), _act_type(D), n, _ld(D), _ptr(groups.inverse), _ptr(weights), T, top, N,
+        _check(spense_combine_rows(_ptr(D), _act_type(D), n, _ld(D), groups.inverse_ptr, _ptr(weights), T, top, N,
                                    _ptr(out), _ld(out), SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, _stream(dev)))
     return out
 
@@ -1051,7 +1079,7 @@ class AdapterPool:
         self.count, self.R, self.K = A.shape
         self.N = B.shape[1]
         self.device = A.device
-        _on_gpu(self.device, B=B)
+        _on_gpu(self.device, B)
         _check_scale(scale, self.count, self.device, "scale")
         self.A, self.B, self.scale = A, B, scale
         self.desc = spense_adapters_t(self.count, self.R, self.K, self.N, _ptr(A), _ptr(B), _ptr(scale))
@@ -1076,13 +1104,14 @@ def add_adapters(base: torch.Tensor, X: torch.Tensor, pool: AdapterPool, groups:
     bt = _act_type(base)
     if groups.n != M or groups.groups != pool.count:
         raise ValueError(f"groups are of {groups.n} rows over {groups.groups}, expected {M} over {pool.count}")
-    _on_gpu(dev, base=base, pool=pool.A, groups=groups.order)
+    _on_gpu(dev, base, pool.A)
+    _same_device(groups, dev)
     _check_scale(x_scale, M, dev, "x_scale")
     out = _out(out, M, pool.N, out_f32, dev)
     ws = workspace or _CallScratch(dev)
     with _device(dev):
         wp, wn = ws.get(spense_adapters_workspace_size(M, pool.desc))
-        _check(spense_add_adapters(_ptr(X), xt, M, _ld(X), _ptr(x_scale), _ptr(groups.order), _ptr(groups.offsets),
+        _check(spense_add_adapters(_ptr(X), xt, M, _ld(X), _ptr(x_scale), groups.order_ptr, groups.offsets_ptr,
                                    pool.desc, _ptr(base), bt, _ld(base), _ptr(out), _ld(out),
                                    SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, wp, wn, _stream(dev)))
     return out
@@ -1139,13 +1168,13 @@ def _check_experts(X, experts, groups, w_scales, x_scale, top, gathered):
     if top < 1:
         raise ValueError(f"top = {top}")
     dev = X.device
-    _on_gpu(dev, groups=groups.order)
+    _same_device(groups, dev)
     if X.shape[0] * (1 if gathered else top) != groups.n:
         raise ValueError(f"X has {X.shape[0]} rows, the groups {groups.n}")
     for w, s in zip(experts, w_scales):
         if groups.groups != w.count:
             raise ValueError(f"groups are over {groups.groups} experts, the weights over {w.count}")
-        _on_gpu(dev, experts=w.dense)
+        _on_gpu(dev, w.dense)
         if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (w.count, w.N) or not s.is_contiguous()
                               or s.device != dev):
             raise ValueError(f"w_scale must be a contiguous fp32 tensor of shape {(w.count, w.N)} on {dev}")
@@ -1179,8 +1208,8 @@ def gemm_experts(X: torch.Tensor, experts, groups: RowGroups, w_scales=None, x_s
     yarr = (ctypes.c_void_p * k)(*[_ptr(o) for o in outs])
     larr = (ctypes.c_int64 * k)(*[_ld(o) for o in outs])
     with _device(dev):
-        _check(spense_gemm_experts(_ptr(X), X.shape[0], _ld16(X), _ptr(x_scale), None if gathered else _ptr(groups.order),
-                                   top, _ptr(groups.offsets), n, experts[0].count, k, parr, sarr, yarr, larr,
+        _check(spense_gemm_experts(_ptr(X), X.shape[0], _ld16(X), _ptr(x_scale), None if gathered else groups.order_ptr,
+                                   top, groups.offsets_ptr, n, experts[0].count, k, parr, sarr, yarr, larr,
                                    SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, _stream(dev)))
     return outs
 
@@ -1199,7 +1228,7 @@ def gemm_experts_glu_fp8(X: torch.Tensor, gate: PackedExperts, up: PackedExperts
     with _device(dev):
         wp, wn = ws.get(spense_gemm_experts_glu_fp8_workspace_size(n, gate.count, N))
         _check(spense_gemm_experts_glu_fp8(_ptr(X), X.shape[0], _ld16(X), _ptr(x_scale),
-                                           None if gathered else _ptr(groups.order), top, _ptr(groups.offsets), n,
+                                           None if gathered else groups.order_ptr, top, groups.offsets_ptr, n,
                                            gate.count, ctypes.byref(gate.desc), ctypes.byref(up.desc), _ptr(gate_scale),
                                            _ptr(up_scale), _ptr(q), N, _ptr(scales), wp, wn, _stream(dev)))
     return q, scales

@@ -20,6 +20,7 @@ namespace {
 struct ExpertRegion {
   int32_t tile0, row0, rows, mat;
   int32_t n_sp, n_de;  // chunks of 512 columns, 2:4 then dense
+  int32_t wg0;         // experts_stream_kernel: its first workgroup
 };
 
 struct ExpertArgs {
@@ -30,6 +31,7 @@ struct ExpertArgs {
   int32_t K, kbound;  // kbound: the first dense column of an input-split weight, 0 of an output-split one
   int32_t out_f32;
   int32_t tiles, wgs;  // 16-row tiles of all regions, workgroups of a tile of positions
+  int32_t tiles_wave;  // experts_stream_kernel: row tiles of a wave
   int32_t nreg;
   ExpertRegion reg[4];
   MatDesc mat[2];
@@ -138,6 +140,143 @@ __global__ __launch_bounds__(64 * WV) void experts_rows_kernel(ExpertArgs a, Exp
   }
 }
 
+// Where a tile's activations fit LDS whole (16 CT rows x K): copied once behind one barrier, after
+// which each wave streams the weights of its row tiles (`tiles_wave` of them, eight apart) on its
+// own, the next tile's first chunks requested while the last of this one are multiplied.  The start
+// of a workgroup (finding its tile, the activations) is then paid once per eight times tiles_wave row
+// tiles, and a short K does not drain the pipeline between them.  A workgroup's row tiles are of one
+// region.
+constexpr int kStreamTiles = 8;  // most row tiles of a wave
+
+template <int CT>
+__global__ __launch_bounds__(512) void experts_stream_kernel(ExpertArgs a, ExpertRows er) {
+  typedef XTile<kFP8, CT> XT;
+  constexpr int NS = CT <= 2 ? 4 : 3, D = NS - 1, P = CT == 1 ? 4 : 1;
+  constexpr int KC = XT::CHUNK_K, NL = 9;
+  RowTile t;
+  if (!find_tile(er.offsets, er.count, er.n, false, 16 * CT, blockIdx.x / a.wgs, t)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, li = lane & 15, lq = lane >> 4;
+  const int wg = blockIdx.x % a.wgs;
+  int ri = 0;
+  for (int i = 1; i < a.nreg; ++i)
+    if (wg >= a.reg[i].wg0) ri = i;
+  const ExpertRegion& R = a.reg[ri];
+  const MatDesc& MD = a.mat[R.mat];
+  const int64_t e = t.group;
+  const int tiles = (R.rows + 15) / 16, first = (wg - R.wg0) * 8 * a.tiles_wave + wave;  // the wave's row tiles: first, first + 8, ...
+  const int mine = min(a.tiles_wave, (tiles - first + 7) / 8);
+  const int nb = (a.kbound + KC - 1) / KC, chunks = nb + (a.K - a.kbound + KC - 1) / KC;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  float* const lsw = reinterpret_cast<float*>(lds + chunks * XT::BYTES) + wave * (16 * kStreamTiles);  // scales of the wave's rows
+  const __amdgpu_buffer_rsrc_t rx = rsrc(a.X, a.x_bytes), rv = rsrc(MD.values + e * MD.v_bytes, MD.v_bytes),
+                               rm = rsrc(reinterpret_cast<const uint8_t*>(MD.meta) + e * MD.m_bytes, MD.m_bytes),
+                               rd = rsrc(MD.dense + e * MD.d_bytes, MD.d_bytes),
+                               rs = rsrc(MD.sw ? MD.sw + e * er.N : nullptr, MD.sw ? 4u * (uint32_t)er.N : 0u);
+  uint32_t xo[CT];
+  int col[CT];
+#pragma unroll
+  for (int i = 0; i < CT; ++i) {
+    const int byte = (wave * CT + i) * 1024 + 16 * lane, r = byte / XT::ROW_B;
+    col[i] = 16 * (((byte % XT::ROW_B) >> 4) ^ (r & 31));
+    const int src = t.p0 + r < t.p1 ? source_row(er, t.p0 + r) : -1;
+    xo[i] = src >= 0 ? (uint32_t)((int64_t)src * a.ldx_b) + (uint32_t)col[i] : kOOB;
+  }
+  float xs[CT];
+  source_scales<CT>(xs, er, a.sx, t.p0 + li, t.p1);
+  // scales, four row tiles a load: lane l row l % 16 of row tile l / 16
+#pragma unroll
+  for (int i = 0; i < kStreamTiles / 4; ++i) {
+    const int srow = 16 * (first + 8 * (4 * i + lq)) + li;
+    lds_load4<0>(rs, reinterpret_cast<uint8_t*>(lsw + 64 * i), srow < R.rows ? 4u * (uint32_t)(R.row0 + srow) : kOOB, 0);
+  }
+  for (int c = 0; c < chunks; ++c) {
+    const int kc = c < nb ? c * KC : a.kbound + (c - nb) * KC, ke = c < nb ? a.kbound : a.K;
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+      lds_load16<0>(rx, lds + c * XT::BYTES + (wave * CT + i) * 1024, kc + col[i] < ke ? xo[i] : kOOB, kc);
+  }
+  auto run = [&](auto act_const) {
+    constexpr bool ACT = decltype(act_const)::value;
+    WChunk slot[NS][1];
+    // the chunk to request next: chunk lc of the tile at vt, mt, dt
+    int lc = 0, left = mine * chunks;
+    uint32_t vt = (uint32_t)first * (uint32_t)R.n_sp * 4096u + 16u * lane, mt = (uint32_t)first * (uint32_t)R.n_sp * 1024u + 16u * lane,
+             dt = (uint32_t)first * (uint32_t)R.n_de * 8192u + 16u * lane;
+    auto load = [&](WChunk& W) {
+      load_chunk_tiled(W, lc < R.n_sp, left > 0, lc, max(lc - R.n_sp, 0), vt, mt, dt, rv, rm, rd);
+      --left;
+      if (++lc == chunks) {
+        lc = 0;
+        vt += 8u * (uint32_t)R.n_sp * 4096u;
+        mt += 8u * (uint32_t)R.n_sp * 1024u;
+        dt += 8u * (uint32_t)R.n_de * 8192u;
+      }
+    };
+    if constexpr (ACT) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        __builtin_amdgcn_sched_barrier(0);
+        load(slot[d][0]);
+      }
+    }
+    barrier_vm<ACT ? D * NL : 0>();  // every wave's activations and scales have landed
+    if constexpr (ACT) {
+      v4f acc[1][CT];
+#pragma unroll
+      for (int c = 0; c < CT; ++c) acc[0][c] = (v4f){0.f, 0.f, 0.f, 0.f};
+      int cc = 0, r = 0;  // the chunk and tile to multiply
+      auto step = [&](auto s_const) {
+        constexpr int S = decltype(s_const)::value, SD = (S + D) % NS;
+        load(slot[SD][0]);
+        __builtin_amdgcn_sched_barrier(0);
+        mma_chunk<kFP8, CT, 1, true, P>(acc, slot[S], cc < R.n_sp, lds + cc * XT::BYTES, li, lq);
+        __builtin_amdgcn_sched_barrier(0);
+        if (++cc == chunks) {
+          xdl_fence();
+          const int n0 = R.row0 + 16 * (first + 8 * r) + 4 * lq, rowend = R.row0 + R.rows;
+          const v4f w = MD.sw ? *reinterpret_cast<const v4f*>(lsw + 16 * r + 4 * lq) : (v4f){1.f, 1.f, 1.f, 1.f};
+          GemmArgs o;
+          o.out_f32 = a.out_f32;
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            const int p = t.p0 + 16 * c + li;
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = acc[0][c][q] * w[q] * xs[c];
+            if (p < t.p1 && n0 < rowend) put4(MD.Y, MD.ldy, MD.vec_store, o, v, p, n0, rowend);
+            acc[0][c] = (v4f){0.f, 0.f, 0.f, 0.f};
+          }
+          cc = 0;
+          ++r;
+        }
+      };
+      int i = mine * chunks;
+      for (; i >= NS; i -= NS) static_for<NS>([&](auto s_const) { step(s_const); });
+      static_for<NS - 1>([&](auto s_const) {
+        if (decltype(s_const)::value < i) step(s_const);
+      });
+    }
+  };
+  if (mine > 0)
+    run(std::true_type());
+  else
+    run(std::false_type());
+}
+
+template <int CT, int WV>
+hipError_t launch_rows(const ExpertArgs& a, const ExpertRows& er, int64_t grid, hipStream_t s) {
+  hipLaunchKernelGGL((experts_rows_kernel<CT, WV>), dim3((unsigned)grid), dim3(64 * WV), 0, s, a, er);
+  return hipGetLastError();
+}
+
+template <int CT>
+hipError_t launch_stream(const ExpertArgs& a, const ExpertRows& er, int64_t grid, int lds, hipStream_t s) {
+  const hipError_t e = set_big_lds(experts_stream_kernel<CT>, 0, CT, 160 * 1024);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(experts_stream_kernel<CT>, dim3((unsigned)grid), dim3(512), lds, s, a, er);
+  return hipGetLastError();
+}
+
 }  // namespace
 }  // namespace spense
 
@@ -150,11 +289,31 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Kernels of the grouped products.
 enum Kernel { kRows16, kRows32, kRows64, kMid, kBig };
 
+// Chunks of 512 columns that experts_stream_kernel takes: up to K = 3072, beyond which waiting for
+// all activations costs more than the pipeline's drains (2048 x 4096, 8 rows an expert: 15.1 us
+// against 10.5; 4096 x 2560 22.3 against 23.9; 5120 x 1536 39 against 48).
+constexpr int64_t kStreamChunks = 6;
+
+// Average rows of an expert from which its tiles are computed 256 x 256 (below: 128 x 128).
+constexpr int64_t kBigRows = 96;
+
+int64_t rows_per_expert(int64_t n, int64_t count) { return n / (count < n ? count : n); }
+
 // The kernel for n rows in count groups: by the rows an expert gets on average where they spread
-// evenly (the counts themselves are on the device).
-Kernel choose_kernel(int64_t n, int64_t count) {
-  const int64_t avg = n / (count < n ? count : n);
-  return avg <= 12 ? kRows16 : avg <= 24 ? kRows32 : avg < 48 ? kRows64 : avg < 192 ? kMid : kBig;
+// evenly (the counts themselves are on the device).  A tile that an expert's rows do not fit costs its
+// weights again, a wider one little, and less with the activations in LDS.  us at 8 / 12 / 20 / 32 /
+// 40 rows an expert, tiles of 16, 32, 64: 32 experts of 5120 x 1536 39 / 58 / 61 / 81 / 102, 41 / 41
+// / 43 / 67 / 71, 42 / 43 / 44 / 48 / 50; 32 of 1536 x 5120 at 12 / 16 / 24 / 32 36 / - / - / -, 40 /
+// 41 / 45 / 64, 43 / 44 / 47 / 49.  Then 48 / 64 / 96 / 128 / 192, tiles of 64, 128 x 128 and 256 x 256:
+// 1536 x 5120 53 / 74 / 86, 55 / 58 / 65 / 100 / 124, 53 / 53 / 57 / 66 / 81; 5120 x 1536 65 / 76 / -,
+// 59 / 62 / 70 / 93 / 119, 66 / 66 / 69 / 74 / 87; 64 experts of 768 x 2048 30 / 42 / 51, 34 / 36 / 52 /
+// 53 / 77, 43 / 46 / 50 / 53 / 63.
+Kernel choose_kernel(int64_t n, int64_t count, int64_t chunks) {
+  const int64_t avg = rows_per_expert(n, count);
+  if (avg >= kBigRows) return kBig;
+  if (avg >= 48) return kMid;
+  const bool stream = chunks <= kStreamChunks;
+  return avg <= (stream ? 8 : 12) ? kRows16 : avg <= (stream ? 18 : 24) ? kRows32 : kRows64;
 }
 
 // One call's checked arguments.
@@ -271,7 +430,7 @@ int launch_tiles(Call& c, bool big, float* pmax, int64_t pmax_ld, hipStream_t st
   return e == hipSuccess ? SPENSE_OK : api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));
 }
 
-int launch_rows(Call& c, int ct, hipStream_t stream) {
+int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
   spense::ExpertArgs a;
   memset(&a, 0, sizeof a);
   a.X = c.X, a.ldx_b = c.ldx, a.x_bytes = (uint32_t)c.xb, a.sx = c.x_scale;
@@ -280,31 +439,54 @@ int launch_rows(Call& c, int ct, hipStream_t stream) {
   int64_t tiles = 0;
   for (int i = 0; i < c.nreg; ++i) {
     a.reg[i] = {(int32_t)tiles, (int32_t)c.reg[i].row0, (int32_t)c.reg[i].rows, c.reg[i].mat,
-                (int32_t)ceil_div(c.reg[i].kbound, 512), (int32_t)ceil_div(c.K - c.reg[i].kbound, 512)};
+                (int32_t)ceil_div(c.reg[i].kbound, 512), (int32_t)ceil_div(c.K - c.reg[i].kbound, 512), 0};
     tiles += ceil_div(c.reg[i].rows, 16);
   }
   a.tiles = (int32_t)tiles;
-  const int wv = ct == 1 ? 4 : 8;
-  a.wgs = (int32_t)ceil_div(tiles, wv);
-  const int64_t grid = spense::most_tiles(c.er.n, c.er.count, false, 16 * ct) * a.wgs;
+  const int64_t most = spense::most_tiles(c.er.n, c.er.count, false, 16 * ct);
+  const int64_t lds = chunks * ct * 8192 + 8 * 16 * spense::kStreamTiles * 4;
+  const bool stream_kernel = chunks <= kStreamChunks && lds <= 160 * 1024;
+  const int wv = stream_kernel ? 8 : ct == 1 ? 4 : 8;
+  if (stream_kernel) {
+    auto wgs = [&](int64_t per) {
+      int64_t w = 0;
+      for (int i = 0; i < c.nreg; ++i) {
+        a.reg[i].wg0 = (int32_t)w;
+        w += ceil_div(ceil_div(c.reg[i].rows, 16), 8 * per);
+      }
+      return w;
+    };
+    // row tiles of a wave: rounds of the 256 CUs (one workgroup each) times a workgroup's time, its
+    // start as long as 90 KB of weights; tiles as even groups would give
+    const int64_t used = c.er.count < c.er.n ? c.er.count : c.er.n, tiles_even = used * ceil_div(c.er.n / used, 16 * ct);
+    const int64_t step = 128 * c.K * 23 / 32;  // bytes of eight row tiles, a quarter of them dense
+    int64_t best = 0;
+    for (int64_t per = 1; per <= spense::kStreamTiles; ++per) {
+      const int64_t cost = ceil_div(tiles_even * wgs(per), 256) * (90000 + per * step);
+      if (per == 1 || cost < best) best = cost, a.tiles_wave = (int32_t)per;
+    }
+    a.wgs = (int32_t)wgs(a.tiles_wave);
+  } else {
+    a.wgs = (int32_t)ceil_div(tiles, wv);
+  }
+  const int64_t grid = most * a.wgs;
   if (grid > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
   int rc = spense::api_check_device();
   if (rc) return rc;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * wv), 0, stream, a, c.er); };
-  if (ct == 1)
-    go(spense::experts_rows_kernel<1, 4>);
-  else if (ct == 2)
-    go(spense::experts_rows_kernel<2, 8>);
-  else
-    go(spense::experts_rows_kernel<4, 8>);
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = stream_kernel ? (ct == 1   ? spense::launch_stream<1>(a, c.er, grid, (int)lds, stream)
+                                        : ct == 2 ? spense::launch_stream<2>(a, c.er, grid, (int)lds, stream)
+                                                  : spense::launch_stream<4>(a, c.er, grid, (int)lds, stream))
+                                     : (ct == 1   ? spense::launch_rows<1, 4>(a, c.er, grid, stream)
+                                        : ct == 2 ? spense::launch_rows<2, 8>(a, c.er, grid, stream)
+                                                  : spense::launch_rows<4, 8>(a, c.er, grid, stream));
   return e == hipSuccess ? SPENSE_OK : api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));
 }
 
 int launch_products(Call& c, hipStream_t stream) {
-  const Kernel k = choose_kernel(c.er.n, c.er.count);
+  const int64_t kbound = c.in_split ? c.db : 0, chunks = ceil_div(kbound, 512) + ceil_div(c.K - kbound, 512);
+  const Kernel k = choose_kernel(c.er.n, c.er.count, chunks);
   if (k >= kMid) return launch_tiles(c, k == kBig, nullptr, 0, stream);
-  return launch_rows(c, k == kRows16 ? 1 : k == kRows32 ? 2 : 4, stream);
+  return launch_few(c, chunks, k == kRows16 ? 1 : k == kRows32 ? 2 : 4, stream);
 }
 
 // The workspace of the gate / up pair: H, or G then U, fp32 with rows padded to 64 elements, and
@@ -341,7 +523,7 @@ int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float*
 
 size_t spense_gemm_experts_glu_fp8_workspace_size(int64_t n, int32_t count, int64_t N) {
   if (n < 1 || n > INT32_MAX || N < 1 || N > INT32_MAX || count < 1 || count > SPENSE_MAX_GROUPS) return 0;
-  if (choose_kernel(n, count) == kBig) return (size_t)(glu_rows_bytes(n, N) + n * glu_maxima(N) * 4);
+  if (rows_per_expert(n, count) >= kBigRows) return (size_t)(glu_rows_bytes(n, N) + n * glu_maxima(N) * 4);
   return (size_t)(2 * glu_rows_bytes(n, N));
 }
 
@@ -367,7 +549,7 @@ int spense_gemm_experts_glu_fp8(const void* X, int64_t rows_x, int64_t ldx, cons
   float* const H = static_cast<float*>(ws);
   float* const second = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + half);
   hipError_t e;
-  if (choose_kernel(n, count) == kBig) {
+  if (rows_per_expert(n, count) >= kBigRows) {
     int64_t blocks = 0;
     for (int i = 0; i < c.nreg; ++i)
       if (c.reg[i].mat == 0) blocks += ceil_div(c.reg[i].rows, 128);

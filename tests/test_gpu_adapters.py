@@ -164,7 +164,7 @@ def test_rows_outside_are_skipped(S):
     order = torch.arange(M, dtype=torch.int32)
     order[3], order[8] = -5, 2 ** 30
     offsets = torch.tensor([-4, 20, 10 ** 9], dtype=torch.int32)
-    g = S.RowGroups(M, 2, order.cuda(), None, offsets.cuda())
+    g = S.RowGroups(M, 2, torch.cat([order, order, offsets]).cuda())
     out = torch.full((M, N), 7.0, device="cuda")
     S.add_adapters(t[5].cuda(), t[0].cuda(), pool, g, out=out, out_f32=True)
     t[6][:], t[6][20:] = 0, 1

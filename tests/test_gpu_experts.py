@@ -193,7 +193,7 @@ def test_rows_outside_give_zeros(S, T):
     x, xs = tokens(g, T, 128, True)
     order = torch.arange(T, dtype=torch.int32)
     order[3], order[8] = -9, 2 ** 31 - 1
-    groups = S.RowGroups(T, 2, order.cuda(), None, torch.tensor([-7, T // 2, 2 ** 31 - 1], dtype=torch.int32, device="cuda"))
+    groups = S.RowGroups(T, 2, torch.cat([order, order, torch.tensor([-7, T // 2, 2 ** 31 - 1], dtype=torch.int32)]).cuda())
     y, = S.gemm_experts(x.view(torch.uint8).cuda(), [pe], groups, [sc.cuda()], xs.cuda(), out_f32=True)
     y = y.cpu()
     assert torch.all(y[3] == 0) and torch.all(y[8] == 0)
