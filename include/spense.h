@@ -580,7 +580,7 @@ int spense_block_norm(const spense_block_norm_t* args, hipStream_t stream);
  *            offsets[groups] is the number of entries in any group;
  *   inverse: n int32 or NULL; the position of each entry, -1 where its idx names no group.
  * idx: n int32 on the device, any values.  Outputs must not overlap idx or each other.  The
- * result depends on idx only.  One workgroup; asynchronous, allocates nothing.
+ * result depends on idx only.  One launch; asynchronous, allocates nothing.
  * SPENSE_ERR_ARG for NULL pointers, n below 0 or above 2^31-1, groups outside [1,
  * SPENSE_MAX_GROUPS].
  */
@@ -616,7 +616,7 @@ typedef struct spense_adapters_t {
 } spense_adapters_t;
 
 /* Device workspace (bytes) of spense_add_adapters for M tokens: fp32 partial sums of A x, up
- * to 16 x M x R of them (0 for a pool or an M that the call refuses). */
+ * to 8 x M x R of them (0 for a pool or an M that the call refuses). */
 size_t spense_adapters_workspace_size(int64_t M, const spense_adapters_t* pool);
 
 /*

@@ -2,8 +2,8 @@
 //   Y[m] = base[m] + s_a * B_a (A_a x_m),  a the adapter of token m (none: Y[m] = base[m]),
 // A_a R x K and B_a N x R in bf16, tokens grouped by adapter (spense_group_rows).
 //
-// Two launches.  The first forms V = s_a x_scale (A_a x) for tiles of 16 or 64 tokens of one
-// adapter on 16x16x32 bf16 matrix instructions, K cut over the four waves of a workgroup and
+// Two launches.  The first forms V = s_a x_scale (A_a x) for tiles of 16 or 32 tokens of one
+// adapter on 16x16x32 bf16 matrix instructions, K cut over the waves of a workgroup and
 // over workgroups; each writes its fp32 partial sums.  The second adds the partials in a fixed
 // order, forms B_a V for the tile and adds it to base on the way to Y.
 //
@@ -39,6 +39,7 @@ struct AdapterArgs {
   int32_t vec;       // base and Y rows in aligned pieces of eight
   int32_t in_place;  // base is Y: rows without an adapter are left alone
   int32_t nblocks;   // second launch: workgroups along N
+  int32_t steps;     // and steps of 128 columns each of them takes
 };
 
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -61,18 +62,20 @@ __device__ __forceinline__ v4f mma_bf16(v4i a, v4i b, v4f c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
 
-// V partials of one tile (CT * 16 tokens), RT * 16 ranks from 16 RT * blockIdx.z and one K
-// slice.  A step is 64 columns: lane group q takes columns [16 q, 16 q + 16) of both operands
+// V partials of one tile (16 CT tokens), RT * 16 ranks from 16 RT * blockIdx.z and one K
+// slice (1, 2, 4 or 8 of them; workgroups of XCD x = blockIdx.x % 8 all take slice x % slices, so that
+// an XCD reads that part of the adapters and activations only).  A step is 64 columns: lane group q takes columns [16 q, 16 q + 16) of both operands
 // (a permutation of K inside the step, the same on both sides), which makes a row's step one
 // 128-byte line of A.
-template <bool FP8, int RT, int CT>
-__global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterArgs a) {
+template <bool FP8, int RT, int CT, int NW>
+__global__ __launch_bounds__(64 * NW) void adapter_shrink_kernel(AdapterArgs a) {
   RowTile t;
-  if (!find_tile(a.offsets, a.count, a.M, false, 16 * CT, blockIdx.x, t)) return;
+  const int x = blockIdx.x & 7, slice = x % a.slices;
+  if (!find_tile(a.offsets, a.count, a.M, false, 16 * CT, (blockIdx.x >> 3) * (8 / a.slices) + x / a.slices, t)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, li = lane & 15, lq = lane >> 4;
   const int r0 = 16 * RT * blockIdx.z;
   const int steps = (a.K + 63) / 64;
-  const int s0 = (int)((int64_t)steps * blockIdx.y / a.slices), s1 = (int)((int64_t)steps * (blockIdx.y + 1) / a.slices);
+  const int s0 = (int)((int64_t)steps * slice / a.slices), s1 = (int)((int64_t)steps * (slice + 1) / a.slices);
   const __amdgpu_buffer_rsrc_t rx = rsrc(a.X, a.x_bytes),
                                ra = rsrc(a.A + (int64_t)t.group * a.R * a.K * 2, (uint32_t)a.R * (uint32_t)a.K * 2u);
   constexpr int XS = FP8 ? 1 : 2;
@@ -95,32 +98,44 @@ __global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterArgs a) {
   for (int r = 0; r < RT; ++r)
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[r][c] = (v4f){0.f, 0.f, 0.f, 0.f};
-  for (int s = s0 + wave; s < s1; s += 4) {
-    const bool in = 64 * s + 16 * lq < a.K;  // K is a multiple of 32
-    v4i av[RT][2], xv[CT][2];
+  for (int s = s0 + wave; s < s1; s += 2 * NW) {  // two steps' loads in flight
+    v4i av[2][RT][2], xv[2][CT][2];
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int u = 0; u < 2; ++u) {
+      const int su = s + u * NW;
+      const bool in = su < s1 && 64 * su + 16 * lq < a.K;  // K is a multiple of 32
 #pragma unroll
-      for (int h = 0; h < 2; ++h) av[r][h] = bl16<0>(ra, sel(in, ao[r] == kOOB ? kOOB : ao[r] + 16u * h), 128 * s);
+      for (int c = 0; c < CT; ++c) {
+        if constexpr (FP8) {
+          xv[u][c][0] = bl16<0>(rx, sel(in, xo[c]), 64 * su);
+        } else {
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      if constexpr (FP8) {
-        codes_to_bf16(bl16<0>(rx, sel(in, xo[c]), 64 * s), xv[c]);
-      } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) xv[c][h] = bl16<0>(rx, sel(in, xo[c] == kOOB ? kOOB : xo[c] + 16u * h), 128 * s);
+          for (int h = 0; h < 2; ++h) xv[u][c][h] = bl16<0>(rx, sel(in, xo[c] == kOOB ? kOOB : xo[c] + 16u * h), 128 * su);
+        }
       }
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) acc[r][c] = mma_bf16(av[r][h], xv[c][h], acc[r][c]);
+        for (int h = 0; h < 2; ++h) av[u][r][h] = bl16<0>(ra, sel(in, ao[r] == kOOB ? kOOB : ao[r] + 16u * h), 128 * su);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (FP8) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c) codes_to_bf16(xv[u][c][0], xv[u][c]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[r][c] = mma_bf16(av[u][r][h], xv[u][c][h], acc[r][c]);
+    }
   }
   xdl_fence();
-  // the four waves' sums in LDS, one token tile at a time; wave r' adds rank tile r'
-  __shared__ v4f red[4 * RT * 64];
+  // the waves' sums in LDS, one token tile at a time; wave r' adds rank tile r'
+  __shared__ v4f red[NW * RT * 64];
   const float sa = a.scale ? a.scale[t.group] : 1.0f;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -131,31 +146,37 @@ __global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterArgs a) {
     if (wave < RT && row[c] >= 0) {
       v4f v = red[wave * 64 + lane];
 #pragma unroll
-      for (int w = 1; w < 4; ++w) v += red[(w * RT + wave) * 64 + lane];
+      for (int w = 1; w < NW; ++w) v += red[(w * RT + wave) * 64 + lane];
       const float f = a.xs ? a.xs[row[c]] : 1.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = v[e] * f * sa;
       const int r = r0 + 16 * wave + 4 * lq;
       if (r < a.R)
-        *reinterpret_cast<v4f*>(a.part + ((int64_t)blockIdx.y * a.M + t.p0 + 16 * c + li) * a.R + r) = v;
+        *reinterpret_cast<v4f*>(a.part + ((int64_t)slice * a.M + t.p0 + 16 * c + li) * a.R + r) = v;
     }
   }
 }
 
+// Eight consecutive bf16 or fp32 values as they lie in memory, and as fp32.
 template <bool BF>
-__device__ __forceinline__ void load8(float (&v)[8], const uint8_t* row, int n) {
-  if constexpr (BF) {
-    const u4 d = *reinterpret_cast<const u4*>(row + 2 * (int64_t)n);
+struct Eight {
+  v4i d[BF ? 1 : 2];
+};
+
+template <bool BF>
+__device__ __forceinline__ Eight<BF> load8(const uint8_t* row, int n) {
+  Eight<BF> v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? d[e / 2] & 0xffff0000u : d[e / 2] << 16);
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const v4f d = *reinterpret_cast<const v4f*>(row + 4 * (int64_t)n + 16 * h);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * h + e] = d[e];
-    }
-  }
+  for (int h = 0; h < (BF ? 1 : 2); ++h) v.d[h] = *reinterpret_cast<const v4i*>(row + (BF ? 2 : 4) * (int64_t)n + 16 * h);
+  return v;
+}
+
+template <bool BF>
+__device__ __forceinline__ float value(const Eight<BF>& v, int e) {
+  if constexpr (BF)
+    return __uint_as_float(e & 1 ? (uint32_t)v.d[0][e / 2] & 0xffff0000u : (uint32_t)v.d[0][e / 2] << 16);
+  else
+    return __int_as_float(v.d[e / 4][e % 4]);
 }
 
 template <bool BF>
@@ -186,15 +207,18 @@ __device__ __forceinline__ void store1(float v, uint8_t* row, int n) {
     reinterpret_cast<float*>(row)[n] = v;
 }
 
-// Y for one tile and 32 * 4 * kExpandSteps output columns: wave w takes 32 columns at a time.
+// Y for one tile and 128 * a.steps output columns: wave w takes 32 columns at a time.
 // The rows of the two 16-row matrix products of a step are dealt so that lane (token, q) ends
 // with eight consecutive outputs, columns 8 q .. 8 q + 7 of the 32.  The product's k index runs
-// over hi of all R ranks, then lo of all R; lane group q of instruction j holds ranks 8 (4 j +
-// q) mod R on.
-constexpr int kExpandSteps = 4;
-
+// over hi of all ranks, then lo: for R <= 16 both in one instruction (lane group q holds eight
+// ranks, block q mod R / 8), else lo in the second half of the KS instructions, on the same
+// fragments of B.  V's fragments stay in LDS: in registers they would leave two waves a SIMD (64
+// tokens, R = 64), too few loads in flight.  A step's B and base are requested before V is
+// there (the first U steps') or U steps ahead, without branches a lane takes by itself.
 template <bool BBF, bool YBF, int KS, int CT>
 __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
+  constexpr int U = CT == 1 ? 2 : 1;             // steps requested together (a.steps is even)
+  constexpr int KB = KS == 1 ? 1 : KS / 2;       // fragments of B
   RowTile t;
   if (!find_tile(a.offsets, a.count, a.M, true, 16 * CT, blockIdx.x / a.nblocks, t)) return;
   const bool none = t.group == a.count;
@@ -202,20 +226,62 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, li = lane & 15, lq = lane >> 4;
   __shared__ v4i vfrag[CT * KS * 64];
   const int rb = a.R / 8;
-  if (!none) {
+  const __amdgpu_buffer_rsrc_t rw =
+      rsrc(a.B + (int64_t)(none ? 0 : t.group) * a.N * a.R * 2, none ? 0u : (uint32_t)a.N * (uint32_t)a.R * 2u);
+  const int n_wg = (blockIdx.x % a.nblocks) * 128 * a.steps;
+  int row[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int p = t.p0 + 16 * c + li;
+    row[c] = p < t.p1 ? a.order[p] : -1;
+    if (row[c] >= a.M) row[c] = -1;
+  }
+  v4i bw[U][2][KB];
+  auto load_b = [&](v4i (&w)[2][KB], int s) {
+    const int n0 = n_wg + 32 * (4 * s + wave);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int n = n0 + 8 * (li >> 2) + 4 * i + (li & 3);
+#pragma unroll
+      for (int j = 0; j < KB; ++j) {
+        const int b = KS == 1 && lq >= rb ? lq - rb : 4 * j + lq;  // eight ranks
+        w[i][j] = bl16<0>(rw, sel(n < a.N && b < rb, (uint32_t)n * (uint32_t)a.R * 2u + 16u * (uint32_t)b));
+      }
+    }
+  };
+  // base of token tile c in step s; tokens there are none of read row 0 and are not written
+  auto load_base = [&](int s, int c) {
+    return load8<BBF>(a.base + (int64_t)max(row[c], 0) * a.ldb_b, n_wg + 32 * (4 * s + wave) + 8 * lq);
+  };
+  // whole pieces of eight for every lane of the step (the same for all of the wave)
+  auto whole = [&](int s) { return a.vec && n_wg + 32 * (4 * s + wave) + 32 <= a.N; };
+  Eight<BBF> ob[U][CT];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    load_b(bw[u], u);
+    if (whole(u)) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) ob[u][c] = load_base(u, c);
+    }
+  }
+  {
     for (int f = wave; f < CT * KS; f += 4) {
-      const int c = f / KS, b = 4 * (f % KS) + lq;  // eight of the 2 R virtual ranks
+      const int c = f / KS, j = f % KS;
+      const bool lo = KS == 1 ? lq >= rb : j >= KB;
+      const int b = KS == 1 ? (lo ? lq - rb : lq) : 4 * (j % KB) + lq;  // eight ranks
       const int p = t.p0 + 16 * c + li;
       v4i w = {0, 0, 0, 0};
-      if (b < 2 * rb && p < t.p1) {
+      if (!none && b < rb && p < t.p1) {
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+        const float* pp = a.part + (int64_t)p * a.R + 8 * b;
+        const int64_t slice = (int64_t)a.M * a.R;
+#pragma unroll 4
         for (int s = 0; s < a.slices; ++s) {
-          const float* pp = a.part + ((int64_t)s * a.M + p) * a.R + 8 * (b < rb ? b : b - rb);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const v4f d = *reinterpret_cast<const v4f*>(pp + 4 * h);
+            const v4f d = *reinterpret_cast<const v4f*>(pp + s * slice + 4 * h);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[4 * h + e] += d[e];
           }
@@ -225,7 +291,7 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
           const uint32_t hi = bf16_bits(v[e]);
           const float hf = __uint_as_float(hi << 16);
           // what hi leaves; nothing where hi is infinite or NaN
-          const uint32_t bits = b < rb ? hi : (fabsf(hf) <= 3.3895314e38f ? bf16_bits(v[e] - hf) : 0u);
+          const uint32_t bits = !lo ? hi : (fabsf(hf) <= 3.3895314e38f ? bf16_bits(v[e] - hf) : 0u);
           w[e / 2] |= (int)(bits << (16 * (e & 1)));
         }
       }
@@ -233,124 +299,106 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
     }
     __syncthreads();
   }
-  v4i vf[CT][KS];
+  for (int s0 = 0; s0 < a.steps; s0 += U) {
 #pragma unroll
-  for (int c = 0; c < CT; ++c)
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + u;
+      const int n0 = n_wg + 32 * (4 * s + wave), nq = n0 + 8 * lq;
+      if (n0 >= a.N) return;
+      const bool full = whole(s);
+      v4f acc[CT][2];
 #pragma unroll
-    for (int j = 0; j < KS; ++j) vf[c][j] = none ? (v4i){0, 0, 0, 0} : vfrag[(c * KS + j) * 64 + lane];
-  int row[CT];
+      for (int c = 0; c < CT; ++c) {
+        acc[c][0] = acc[c][1] = (v4f){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int p = t.p0 + 16 * c + li;
-    row[c] = p < t.p1 ? a.order[p] : -1;
-    if (row[c] >= a.M) row[c] = -1;
-  }
-  const __amdgpu_buffer_rsrc_t rw =
-      rsrc(a.B + (int64_t)(none ? 0 : t.group) * a.N * a.R * 2, none ? 0u : (uint32_t)a.N * (uint32_t)a.R * 2u);
-  const int n_wg = (blockIdx.x % a.nblocks) * 128 * kExpandSteps;
-#pragma unroll 2
-  for (int s = 0; s < kExpandSteps; ++s) {
-    const int n0 = n_wg + 32 * (4 * s + wave);
-    if (n0 >= a.N) break;
-    v4i bw[2][KS];
+        for (int j = 0; j < KS; ++j) {
+          const v4i vf = vfrag[(c * KS + j) * 64 + lane];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int n = n0 + 8 * (li >> 2) + 4 * i + (li & 3);
-#pragma unroll
-      for (int j = 0; j < KS; ++j) {
-        const int b = 4 * j + lq;
-        bw[i][j] = bl16<0>(rw, sel(n < a.N && b < 2 * rb, (uint32_t)n * (uint32_t)a.R * 2u + 16u * (uint32_t)(b < rb ? b : b - rb)));
+          for (int i = 0; i < 2; ++i) acc[c][i] = mma_bf16(bw[u][i][j % KB], vf, acc[c][i]);
+        }
       }
-    }
-    const int nq = n0 + 8 * lq;
-    const bool whole = a.vec && nq + 8 <= a.N;
-    float o[CT][8];
+      xdl_fence();
+      if (s0 + U < a.steps) load_b(bw[u], s + U);
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const uint8_t* br = a.base + (int64_t)(row[c] < 0 ? 0 : row[c]) * a.ldb_b;
-      if (whole && row[c] >= 0) {
-        load8<BBF>(o[c], br, nq);
-      } else {
+      for (int c = 0; c < CT; ++c) {
+        uint8_t* yr = a.Y + (int64_t)row[c] * a.ldy_b;
+        if (full) {
+          float o[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[c][e] = row[c] >= 0 && nq + e < a.N ? load1<BBF>(br, nq + e) : 0.0f;
+          for (int e = 0; e < 8; ++e) o[e] = none ? value<BBF>(ob[u][c], e) : value<BBF>(ob[u][c], e) + acc[c][e / 4][e % 4];
+          if (row[c] >= 0) store8<YBF>(o, yr, nq);
+        } else if (row[c] >= 0) {
+          const uint8_t* br = a.base + (int64_t)row[c] * a.ldb_b;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (nq + e >= a.N) continue;
+            const float o = load1<BBF>(br, nq + e);
+            store1<YBF>(none ? o : o + acc[c][e / 4][e % 4], yr, nq + e);
+          }
+        }
       }
-    }
-    v4f acc[CT][2];
+      if (s0 + U < a.steps && whole(s + U)) {
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        acc[c][i] = (v4f){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < KS; ++j) acc[c][i] = mma_bf16(bw[i][j], vf[c][j], acc[c][i]);
-      }
-    xdl_fence();
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      if (row[c] < 0) continue;
-      uint8_t* yr = a.Y + (int64_t)row[c] * a.ldy_b;
-      if (!none) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[c][4 * i + e] += acc[c][i][e];
-      }
-      if (whole) {
-        store8<YBF>(o[c], yr, nq);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (nq + e < a.N) store1<YBF>(o[c][e], yr, nq + e);
+        for (int c = 0; c < CT; ++c) ob[u][c] = load_base(s + U, c);
       }
     }
   }
 }
 
-// Tokens of a tile: 64 where the batch holds many tokens per adapter, so that A and B rows feed
-// four matrix instructions a load; 16 where it does not (a tile holds one adapter's tokens).
-int tile_tokens(int64_t M, int32_t count, int32_t R) { return R <= 64 && M >= 32 * (int64_t)count && M >= 128 ? 64 : 16; }
+// Tokens of a tile: 64 (32 in the first launch, whose K leaves more to do per token) where the batch
+// holds many tokens per adapter, so that A and B rows feed several matrix instructions a load; 16
+// where it does not (a tile holds one adapter's tokens).
+bool many_tokens(int64_t M, int32_t count, int32_t R) { return R <= 64 && M >= 32 * (int64_t)count && M >= 128; }
+int shrink_tokens(int64_t M, int32_t count, int32_t R) { return many_tokens(M, count, R) ? 32 : 16; }
+int expand_tokens(int64_t M, int32_t count, int32_t R) { return many_tokens(M, count, R) ? 64 : 16; }
 
-// K slices: workgroups for every CU, at least four steps a wave apart from the last.
+// K slices: workgroups for the CUs, each with two rounds of steps or more; but every slice is another
+// M x R of partial sums, which each workgroup along N of the second launch reads again.  us at 2 / 4 / 8
+// slices: M = 2048, R = 64, N = 8192 55 / 63 / 71 (80 workgroups a slice), M = 1000, R = 32, N = 16384
+// 35 / 31 / 35 (35); at 8 / 16, M = 64, R = 16, N = 25600 16.8 / 17.3, M = 256, N = 8192 11.8 / 12.8.
 int k_slices(int64_t M, int32_t count, int64_t K, int32_t R) {
-  const int64_t T = tile_tokens(M, count, R), wg = most_tiles(M, count, false, T) * ((R + 63) / 64);
-  int64_t s = (512 + wg - 1) / wg;
-  const int64_t most = (K + 511) / 512;
+  const bool many = many_tokens(M, count, R);
+  const int64_t wg = most_tiles(M, count, false, shrink_tokens(M, count, R)) * ((R + 63) / 64);
+  int64_t s = ((many ? 160 : 512) + wg - 1) / wg;
+  const int64_t cap = many ? 4 : 8, most = (K + 511) / 512;
   s = s < most ? s : most;
-  return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+  s = s < cap ? s : cap;
+  return s >= 8 ? 8 : s >= 4 ? 4 : s >= 2 ? 2 : 1;
 }
 
 template <bool FP8, int CT>
 void launch_shrink(const AdapterArgs& a, int64_t tiles, hipStream_t st) {
+  constexpr int NW = CT == 2 ? 8 : 4;
   auto go = [&](auto kernel, int rt) {
-    const dim3 grid((unsigned)tiles, (unsigned)a.slices, (unsigned)((a.R + 16 * rt - 1) / (16 * rt)));
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+    const int64_t per = 8 / a.slices;  // tiles of eight workgroups
+    const dim3 grid((unsigned)((tiles + per - 1) / per * 8), 1, (unsigned)((a.R + 16 * rt - 1) / (16 * rt)));
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), 0, st, a);
   };
   if (a.R <= 16)
-    go(adapter_shrink_kernel<FP8, 1, CT>, 1);
+    go(adapter_shrink_kernel<FP8, 1, CT, NW>, 1);
   else if (a.R <= 32)
-    go(adapter_shrink_kernel<FP8, 2, CT>, 2);
+    go(adapter_shrink_kernel<FP8, 2, CT, NW>, 2);
   else
-    go(adapter_shrink_kernel<FP8, 4, CT>, 4);
+    go(adapter_shrink_kernel<FP8, 4, CT, NW>, 4);
 }
 
 template <bool BBF, bool YBF>
 void launch_expand(const AdapterArgs& a, int T, int64_t tiles, hipStream_t st) {
   const dim3 grid((unsigned)(tiles * a.nblocks));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
-  const int ks = (2 * a.R + 31) / 32;
   if (T == 64) {
-    if (ks <= 1)
+    if (a.R <= 16)
       go(adapter_expand_kernel<BBF, YBF, 1, 4>);
-    else if (ks <= 2)
+    else if (a.R <= 32)
       go(adapter_expand_kernel<BBF, YBF, 2, 4>);
     else
       go(adapter_expand_kernel<BBF, YBF, 4, 4>);
   } else {
-    if (ks <= 1)
+    if (a.R <= 16)
       go(adapter_expand_kernel<BBF, YBF, 1, 1>);
-    else if (ks <= 2)
+    else if (a.R <= 32)
       go(adapter_expand_kernel<BBF, YBF, 2, 1>);
-    else if (ks <= 4)
+    else if (a.R <= 64)
       go(adapter_expand_kernel<BBF, YBF, 4, 1>);
     else
       go(adapter_expand_kernel<BBF, YBF, 8, 1>);
@@ -406,9 +454,15 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   const int64_t xb = ((M - 1) * ldx + P.K) * xs;
   if (xb >= lim) return api_fail(SPENSE_ERR_ARG, "X spans 2 GiB or more");
   if (P.K * P.R * 2 >= lim || P.N * P.R * 2 >= lim) return api_fail(SPENSE_ERR_ARG, "an adapter spans 2 GiB or more");
-  const int T = spense::tile_tokens(M, P.count, P.R);
-  const int64_t nblocks = (P.N + 128 * spense::kExpandSteps - 1) / (128 * spense::kExpandSteps);
-  const int64_t tiles = spense::most_tiles(M, P.count, false, T), all_tiles = spense::most_tiles(M, P.count, true, T);
+  const int T = spense::expand_tokens(M, P.count, P.R), Ts = spense::shrink_tokens(M, P.count, P.R);
+  const int64_t tiles = spense::most_tiles(M, P.count, false, Ts), all_tiles = spense::most_tiles(M, P.count, true, T);
+  // columns a workgroup: 1024 where that leaves workgroups enough, their start (the tile, V) then paid
+  // less often, else 256; 512 in tiles of 64.  us at 256 / 512 / 1024: M = 64 over 28 adapters, N =
+  // 25600 18.9 / 17.3 / 15.4; M = 1 7.9 / 8.6 / 10.0, M = 128 over 8, N = 8192 9.6 / 10.3 / 12.6; M =
+  // 2048, N = 8192 in tiles of 64 55.6 / 52.3 / 58.9.
+  const int64_t tiles_used = P.count < M ? P.count : M;
+  const int steps = T == 64 ? 4 : tiles_used * ((P.N + 1023) / 1024) >= 512 ? 8 : 2;
+  const int64_t nblocks = (P.N + 128 * steps - 1) / (128 * steps);
   if (all_tiles * nblocks > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "M x N too large for the grid");
   const size_t need = spense_adapters_workspace_size(M, pool);
   if (!ws || ws_bytes < need) return api_fail(SPENSE_ERR_WS, "workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
@@ -428,10 +482,11 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   a.vec = at(base) % 16 == 0 && a.ldb_b % 16 == 0 && at(Y) % 16 == 0 && a.ldy_b % 16 == 0;
   a.in_place = same;
   a.nblocks = (int32_t)nblocks;
+  a.steps = steps;
   if (x_type == SPENSE_FP8_E4M3FN)
-    T == 64 ? spense::launch_shrink<true, 4>(a, tiles, stream) : spense::launch_shrink<true, 1>(a, tiles, stream);
+    Ts == 32 ? spense::launch_shrink<true, 2>(a, tiles, stream) : spense::launch_shrink<true, 1>(a, tiles, stream);
   else
-    T == 64 ? spense::launch_shrink<false, 4>(a, tiles, stream) : spense::launch_shrink<false, 1>(a, tiles, stream);
+    Ts == 32 ? spense::launch_shrink<false, 2>(a, tiles, stream) : spense::launch_shrink<false, 1>(a, tiles, stream);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) {
     if (bs == 2)

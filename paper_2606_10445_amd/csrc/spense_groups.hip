@@ -1,14 +1,13 @@
 // Rows grouped by an index (expert or adapter), and the rows of a token's experts summed back.
 //
-// Grouping is a stable counting sort in one workgroup: each wave counts the keys of its
-// contiguous part of the index array in its own LDS row, the rows' prefix over waves and the
-// counts' prefix over groups give every (wave, group) its first position, and a second walk
-// over the same entries places them.  Inside a step of 64 entries a lane finds the lanes with
-// its key by ballots over the key's bits; its rank is the number of lower ones.  No atomics:
-// the order is the index order, whatever the timing.
+// Grouping is a stable counting sort in one launch whose workgroups do not wait for each other: a
+// workgroup places 1024 consecutive entries, one a thread, and counts the keys of all n for itself
+// (those before its entries and those after, with LDS additions: whole numbers, the same in any
+// order).  Inside a wave a lane finds the lanes with its key by ballots over the key's bits; its
+// rank is the number of lower ones.  The order is the index order, whatever the timing.
 //
-// Latency-bound: n = 64 to 512 takes one step a wave and pass; every further 1024 entries
-// (512 above 511 groups) one more.
+// Latency-bound at decode sizes (n = 64: 3.9 us).  One workgroup walking all entries with ballots
+// took 22 us for n = 16384, its one CU's vector instructions the bound.
 #include <hip/hip_runtime.h>
 
 #include "spense.h"
@@ -20,60 +19,61 @@ namespace {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-// LDS traffic of other lanes of this wave happens between the statements around it.
-__device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
+constexpr int kGroupThreads = 1024, kGroupWaves = kGroupThreads / 64;
 
-// NW waves, GMAX keys (the groups and one for entries outside them).
-template <int NW, int GMAX>
-__global__ __launch_bounds__(64 * NW) void group_rows_kernel(const int32_t* __restrict__ idx, int64_t n, int groups, int bits,
-                                                             int32_t* __restrict__ order, int32_t* __restrict__ inverse,
-                                                             int32_t* __restrict__ offsets) {
-  __shared__ int cnt[NW][GMAX];
-  __shared__ int base[GMAX];
-  __shared__ int wsum[NW];
+__global__ __launch_bounds__(kGroupThreads) void group_rows_kernel(const int32_t* __restrict__ idx, int64_t n, int groups,
+                                                                   int bits, int32_t* __restrict__ order,
+                                                                   int32_t* __restrict__ inverse,
+                                                                   int32_t* __restrict__ offsets) {
+  constexpr int kKeys = SPENSE_MAX_GROUPS + 1;  // the groups and one for entries outside them
+  __shared__ int before[kKeys], after[kKeys];   // entries with each key before this workgroup's, and from there on
+  __shared__ uint16_t cnt[kGroupWaves][kKeys];  // this workgroup's, by wave
+  __shared__ int wsum[kGroupWaves], carry;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t part = ((n + NW - 1) / NW + 63) / 64 * 64;  // entries of a wave
-  const int64_t i0 = wave * part, i1 = min(n, i0 + part);
-  for (int g = threadIdx.x; g < NW * GMAX; g += 64 * NW) (&cnt[0][0])[g] = 0;
-  __syncthreads();
-  // lanes of this wave with this lane's key (its own included); all lanes take part
-  auto peers = [&](int key) {
-    uint64_t m = ~0ull;
-    for (int b = 0; b < bits; ++b) {
-      const uint64_t set = __ballot((key >> b) & 1);
-      m &= (key >> b) & 1 ? set : ~set;
-    }
-    return m;
-  };
-  auto key_of = [&](int64_t i) {  // entries past the part get the key `groups` and are masked
-    const int v = i < i1 ? idx[i] : -1;
+  const int64_t mine = (int64_t)blockIdx.x * kGroupThreads + threadIdx.x, start = (int64_t)blockIdx.x * kGroupThreads;
+  for (int g = threadIdx.x; g <= groups; g += kGroupThreads) {
+    before[g] = after[g] = 0;
+#pragma unroll
+    for (int w = 0; w < kGroupWaves; ++w) cnt[w][g] = 0;
+  }
+  if (threadIdx.x == 0) carry = 0;
+  auto key_of = [&](int64_t i) {
+    const int v = idx[i];
     return v >= 0 && v < groups ? v : groups;
   };
-  const uint64_t below = (1ull << lane) - 1;
-  int key = key_of(i0 + lane);
-  for (int64_t i = i0; i < i1; i += 64) {
-    const int next = key_of(i + 64 + lane);
-    const uint64_t m = peers(key) & __ballot(i + lane < i1);
-    if (i + lane < i1 && !(m & below)) cnt[wave][key] += __popcll(m);
-    wave_fence();
-    key = next;
-  }
+  const bool in = mine < n;
+  const int key = in ? key_of(mine) : groups;
   __syncthreads();
-  // prefix over the waves of each key, then over the keys
-  for (int g0 = 0; g0 <= groups; g0 += 64 * NW) {
-    const int g = g0 + threadIdx.x;
-    int tot = 0;
-    if (g <= groups) {
-      for (int w = 0; w < NW; ++w) {
-        const int c = cnt[w][g];
-        cnt[w][g] = tot;
-        tot += c;
+  constexpr int kBatch = 8;  // loads in flight
+  for (int64_t i = threadIdx.x; i - threadIdx.x < n; i += kBatch * kGroupThreads) {
+    int k[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) k[u] = i + u * kGroupThreads < n ? key_of(i + u * kGroupThreads) : -1;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      int* const part = i - lane + u * kGroupThreads < start ? before : after;  // a wave's entries are all on one side
+      const int one = __builtin_amdgcn_readfirstlane(k[u]);
+      if (__ballot(k[u] == one) == ~0ull) {  // one key in the whole wave: one addition
+        if (one >= 0 && lane == 0) atomicAdd(&part[one], 64);
+      } else if (k[u] >= 0) {
+        atomicAdd(&part[k[u]], 1);
       }
     }
-    int inc = tot;  // inclusive prefix over the workgroup
+  }
+  // lanes of this wave with this lane's key (its own included); all lanes take part
+  uint64_t peers = __ballot(in);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t set = __ballot((key >> b) & 1);
+    peers &= (key >> b) & 1 ? set : ~set;
+  }
+  const uint64_t lower = peers & ((1ull << lane) - 1);
+  if (in && !lower) cnt[wave][key] = (uint16_t)__popcll(peers);
+  __syncthreads();
+  // before[g]: this workgroup's first position of key g; cnt: of each wave's first, from there
+  for (int g0 = 0; g0 <= groups; g0 += kGroupThreads) {
+    const int g = g0 + threadIdx.x;
+    const int tot = g <= groups ? before[g] + after[g] : 0;
+    int inc = tot;  // inclusive prefix over the keys
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int u = __shfl_up(inc, o, 64);
@@ -81,27 +81,27 @@ __global__ __launch_bounds__(64 * NW) void group_rows_kernel(const int32_t* __re
     }
     if (lane == 63) wsum[wave] = inc;
     __syncthreads();
-    int before = g0 ? base[g0 - 1] : 0;  // base[g]: the entries with keys up to g
-    for (int w = 0; w < wave; ++w) before += wsum[w];
-    if (g <= groups) base[g] = before + inc;
+    int base = carry + inc - tot;
+    for (int w = 0; w < wave; ++w) base += wsum[w];
+    __syncthreads();
+    if (threadIdx.x == kGroupThreads - 1) carry = base + tot;
+    if (g <= groups) {
+      if (blockIdx.x == 0) offsets[g] = base;
+      before[g] += base;
+      int sum = 0;
+#pragma unroll
+      for (int w = 0; w < kGroupWaves; ++w) {
+        const int c = cnt[w][g];
+        cnt[w][g] = (uint16_t)sum;
+        sum += c;
+      }
+    }
     __syncthreads();
   }
-  for (int g = threadIdx.x; g <= groups; g += 64 * NW) offsets[g] = g ? base[g - 1] : 0;
-  key = key_of(i0 + lane);
-  for (int64_t i = i0; i < i1; i += 64) {
-    const int next = key_of(i + 64 + lane);
-    const bool in = i + lane < i1;
-    const uint64_t m = peers(key) & __ballot(in);
-    const int first = cnt[wave][key];
-    wave_fence();
-    if (in && !(m & below)) cnt[wave][key] = first + __popcll(m);
-    wave_fence();
-    if (in) {
-      const int p = (key ? base[key - 1] : 0) + first + __popcll(m & below);
-      order[p] = (int32_t)(i + lane);
-      if (inverse) inverse[i + lane] = key < groups ? p : -1;
-    }
-    key = next;
+  if (in) {
+    const int p = before[key] + cnt[wave][key] + __popcll(lower);
+    order[p] = (int32_t)mine;
+    if (inverse) inverse[mine] = key < groups ? p : -1;
   }
 }
 
@@ -189,12 +189,9 @@ int spense_group_rows(const int32_t* idx, int64_t n, int32_t groups, int32_t* or
   if (rc) return rc;
   int bits = 1;
   while ((groups >> bits) != 0) ++bits;  // keys 0 .. groups
-  if (groups < 512)
-    hipLaunchKernelGGL((spense::group_rows_kernel<16, 512>), dim3(1), dim3(1024), 0, stream, idx, n, groups, bits, order,
-                       inverse, offsets);
-  else
-    hipLaunchKernelGGL((spense::group_rows_kernel<8, SPENSE_MAX_GROUPS + 1>), dim3(1), dim3(512), 0, stream, idx, n, groups,
-                       bits, order, inverse, offsets);
+  const int64_t blocks = n > 0 ? (n + spense::kGroupThreads - 1) / spense::kGroupThreads : 1;
+  hipLaunchKernelGGL(spense::group_rows_kernel, dim3((unsigned)blocks), dim3(spense::kGroupThreads), 0, stream, idx, n, groups,
+                     bits, order, inverse, offsets);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return api_fail(SPENSE_ERR_HIP, "group rows launch failed: %s", hipGetErrorString(e));
   return spense::api_ok();

@@ -24,8 +24,11 @@ __device__ __forceinline__ bool find_tile(const int32_t* __restrict__ offsets, i
     a = min(max(offsets[e], 0), n);
     b = e < count ? max(min(max(offsets[e + 1], 0), n), a) : n;
   };
-  int sum = 0;
-  for (int i = 0; i < per; ++i) {
+  int a0 = 0, b0 = 0, sum = 0;  // the lane's first group; its tiles
+  if (lane * per < groups) segment(lane * per, a0, b0);
+  sum = (b0 - a0 + T - 1) / T;
+  const int first = sum;
+  for (int i = 1; i < per; ++i) {
     const int e = lane * per + i;
     if (e < groups) {
       int a, b;
@@ -41,15 +44,16 @@ __device__ __forceinline__ bool find_tile(const int32_t* __restrict__ offsets, i
   }
   const uint64_t mine = __ballot(g >= inc - sum && g < inc);
   if (!mine) return false;
-  int at = g - (inc - sum), e = 0, p0 = 0, p1 = 0;
-  bool found = false;
-  for (int i = 0; i < per; ++i) {
+  int at = g - (inc - sum), e = lane * per, p0 = a0 + at * T, p1 = min(b0, p0 + T);
+  bool found = at < first;
+  at -= first;
+  for (int i = 1; i < per; ++i) {
     const int f = lane * per + i;
     if (f < groups && !found) {
       int a, b;
       segment(f, a, b);
       const int tiles = (b - a + T - 1) / T;
-      if (at >= 0 && at < tiles) {
+      if (at < tiles) {
         e = f, p0 = a + at * T, p1 = min(b, p0 + T);
         found = true;
       }
