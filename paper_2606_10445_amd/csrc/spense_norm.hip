@@ -33,7 +33,7 @@ struct NormArgs {
   const uint8_t* wpre;   // NULL: ones
   int32_t w_bf16;
   float alpha, eps;
-  int64_t K;
+  int64_t M, K;
   uint8_t* r;  // NULL: not written
   int64_t ldr_b;
   uint8_t* n;  // NULL: not written
@@ -49,87 +49,166 @@ __device__ __forceinline__ uint32_t f32_bf16(float v) {
   return (uint32_t)__builtin_bit_cast(uint16_t, h);
 }
 
-// E = 8: elements k .. k + 7, 16-byte aligned; E = 1: element k.
-template <bool BF, int E>
-__device__ __forceinline__ void load_vals(float (&v)[E], const uint8_t* row, int64_t k) {
-  if constexpr (E == 1) {
-    if constexpr (BF)
-      v[0] = bf16_f32(reinterpret_cast<const uint16_t*>(row)[k]);
-    else
-      v[0] = reinterpret_cast<const float*>(row)[k];
-  } else if constexpr (BF) {
-    const v4i a = *reinterpret_cast<const v4i*>(row + 2 * k);
+// Eight elements from column k of a row.  AL: 16-byte aligned (8 for codes) and K a multiple of 8;
+// else the same wide accesses at the alignment of the elements.
+template <int ALIGN>
+struct Wide;
+template <>
+struct Wide<16> {
+  typedef int type __attribute__((ext_vector_type(4), aligned(16)));
+};
+template <>
+struct Wide<4> {
+  typedef int type __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <>
+struct Wide<2> {
+  typedef int type __attribute__((ext_vector_type(4), aligned(2)));
+};
+template <bool AL>
+struct Codes {
+  typedef int type __attribute__((ext_vector_type(2), aligned(8)));
+};
+template <>
+struct Codes<false> {
+  typedef int type __attribute__((ext_vector_type(2), aligned(1)));
+};
+
+template <bool BF, bool AL>
+__device__ __forceinline__ void load8(float (&v)[8], const uint8_t* row, int64_t k) {
+  typedef typename Wide<AL ? 16 : BF ? 2 : 4>::type W;
+  if constexpr (BF) {
+    const W a = *reinterpret_cast<const W*>(row + 2 * k);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e & 1 ? __uint_as_float((uint32_t)a[e / 2] & 0xffff0000u) : bf16_f32((uint32_t)a[e / 2] & 0xffffu);
   } else {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const v4i a = *reinterpret_cast<const v4i*>(row + 4 * k + 16 * h);
+      const W a = *reinterpret_cast<const W*>(row + 4 * k + 16 * h);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[4 * h + e] = __int_as_float(a[e]);
     }
   }
 }
 
-template <bool BF, int E>
-__device__ __forceinline__ void store_vals(const float (&v)[E], uint8_t* row, int64_t k) {
-  if constexpr (E == 1) {
-    if constexpr (BF)
-      reinterpret_cast<uint16_t*>(row)[k] = (uint16_t)f32_bf16(v[0]);
-    else
-      reinterpret_cast<float*>(row)[k] = v[0];
-  } else if constexpr (BF) {
-    v4i a;
+template <bool BF>
+__device__ __forceinline__ float load1(const uint8_t* row, int64_t k) {
+  if constexpr (BF)
+    return bf16_f32(reinterpret_cast<const uint16_t*>(row)[k]);
+  else
+    return reinterpret_cast<const float*>(row)[k];
+}
+
+template <bool BF>
+__device__ __forceinline__ void store1(float v, uint8_t* row, int64_t k) {
+  if constexpr (BF)
+    reinterpret_cast<uint16_t*>(row)[k] = (uint16_t)f32_bf16(v);
+  else
+    reinterpret_cast<float*>(row)[k] = v;
+}
+
+// A piece's elements from column k (of eight) on to a row: all of them, or those from element
+// `from` on.
+template <bool BF, bool AL>
+__device__ __forceinline__ void store8(const float (&v)[8], uint8_t* row, int64_t k, int from) {
+  typedef typename Wide<AL ? 16 : BF ? 2 : 4>::type W;
+  if (from == 0) {
+    if constexpr (BF) {
+      W a;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) a[e] = (int)(f32_bf16(v[2 * e]) | (f32_bf16(v[2 * e + 1]) << 16));
-    *reinterpret_cast<v4i*>(row + 2 * k) = a;
-  } else {
+      for (int e = 0; e < 4; ++e) a[e] = (int)(f32_bf16(v[2 * e]) | (f32_bf16(v[2 * e + 1]) << 16));
+      *reinterpret_cast<W*>(row + 2 * k) = a;
+    } else {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      *reinterpret_cast<v4i*>(row + 4 * k + 16 * h) =
-          (v4i){__float_as_int(v[4 * h]), __float_as_int(v[4 * h + 1]), __float_as_int(v[4 * h + 2]), __float_as_int(v[4 * h + 3])};
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<W*>(row + 4 * k + 16 * h) =
+            (W){__float_as_int(v[4 * h]), __float_as_int(v[4 * h + 1]), __float_as_int(v[4 * h + 2]), __float_as_int(v[4 * h + 3])};
+    }
+  } else if constexpr (!AL) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e >= from) store1<BF>(v[e], row, k + e);
   }
 }
 
-template <int E>
-__device__ __forceinline__ void load_weights(float (&v)[E], const uint8_t* w, int bf, int64_t k) {
+template <bool AL>
+__device__ __forceinline__ void weights8(float (&v)[8], const uint8_t* w, int bf, int64_t k) {
   if (!w) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = 1.0f;
+    for (int e = 0; e < 8; ++e) v[e] = 1.0f;
   } else if (bf) {
-    load_vals<true, E>(v, w, k);
+    load8<true, AL>(v, w, k);
   } else {
-    load_vals<false, E>(v, w, k);
+    load8<false, AL>(v, w, k);
   }
 }
 
-// Codes of v / s (a correctly rounded division; |v / s| rounds to at most 448).
-template <int E>
-__device__ __forceinline__ void store_codes(const float (&v)[E], float s, uint8_t* q, int64_t k) {
-  if constexpr (E == 1) {
-    q[k] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[0] / s, 0.0f, 0, false);
-  } else {
-    typedef int v2i __attribute__((ext_vector_type(2)));
-    v2i w;
+__device__ __forceinline__ float weight1(const uint8_t* w, int bf, int64_t k) {
+  return !w ? 1.0f : bf ? load1<true>(w, k) : load1<false>(w, k);
+}
+
+// v / s for one s and many v, correctly rounded as the division that spense_quantize_fp8 takes, so
+// that the codes are its codes: from y = 1 / s correctly rounded, two steps of Markstein's correction
+// (q + y (v - q s) with exact remainders: the first quotient within an ulp, the second correct), five
+// operations against the division's ten and a reciprocal.  Holds while no remainder underflows: scales
+// outside [2^-60, 2^60] divide; a v below 2^-40 s may be off in its last bits and is a zero code
+// either way, whose sign is v's.  FEW: a thread has too few elements for that to pay (one piece: M = 1,
+// K = 5120 4.8 us against 5.1; two, M = 8192 95.8 against 93.6 with the correction).
+template <bool FEW>
+struct Divisor {
+  float s, y;
+  bool plain;
+  __device__ __forceinline__ explicit Divisor(float s_)
+      : s(s_), y(FEW ? 0.0f : 1.0f / s_), plain(FEW || !(s_ >= 0x1p-60f && s_ <= 0x1p60f)) {}
+  __device__ __forceinline__ float of(float v) const {
+    float q = v * y;
+    q = __builtin_fmaf(__builtin_fmaf(-q, s, v), y, q);
+    q = __builtin_fmaf(__builtin_fmaf(-q, s, v), y, q);
+    return __builtin_copysignf(q, v);
+  }
+};
+
+template <typename D>
+__device__ __forceinline__ uint8_t code1(float v, const D& d) {
+  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(d.plain ? v / d.s : d.of(v), 0.0f, 0, false);
+}
+
+template <bool AL, typename D>
+__device__ __forceinline__ void codes8(const float (&v)[8], const D& d, uint8_t* q, int64_t k, int from) {
+  typedef typename Codes<AL>::type W;
+  if (from == 0) {
+    float t[8];
+    if (d.plain) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = v[e] / d.s;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = d.of(v[e]);
+    }
+    W w;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] / s, v[4 * h + 3] / s,
-                                             __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] / s, v[4 * h + 1] / s, 0, false), true);
-    *reinterpret_cast<v2i*>(q + k) = w;
+      w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(t[4 * h + 2], t[4 * h + 3],
+                                             __builtin_amdgcn_cvt_pk_fp8_f32(t[4 * h], t[4 * h + 1], 0, false), true);
+    *reinterpret_cast<W*>(q + k) = w;
+  } else if constexpr (!AL) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e >= from) q[k + e] = code1(v[e], d);
   }
 }
 
-// Sum or maximum over the workgroup; `red` (16 floats) is used by one reduction only, so one
-// barrier is enough.
-template <bool MAX>
-__device__ __forceinline__ float block_reduce(float v, float* red) {
+// Sum or maximum over L lanes (a power of two up to 64), or with L = 0 over the workgroup; `red`
+// (16 floats) is used by one reduction only, so one barrier is enough.
+template <bool MAX, int L = 0>
+__device__ __forceinline__ float row_reduce(float v, float* red) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
+  for (int o = (L ? L : 64) / 2; o >= 1; o >>= 1) {
     const float u = __shfl_xor(v, o, 64);
     v = MAX ? fmaxf(v, u) : v + u;
   }
   const int nw = blockDim.x >> 6;
-  if (nw == 1) return v;
+  if (L || nw == 1) return v;
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   float s = red[0];
@@ -137,78 +216,85 @@ __device__ __forceinline__ float block_reduce(float v, float* red) {
   return s;
 }
 
-// Rows of up to NJ * E * blockDim.x elements, in registers: thread t owns pieces t + j *
-// blockDim.x of E elements.  K is a multiple of E.
-template <bool XBF, bool YBF, int E, int NJ>
-__global__ __launch_bounds__(1024) void block_norm_kernel(NormArgs a) {
+// Rows of 8 to 8 * NJ * blockDim.x elements, in registers: thread t owns pieces t + j * blockDim.x
+// of eight columns.  A ragged last piece is read as the row's last eight columns, its first `from`
+// of them (the owner of the piece before has them) left out of the sums and stores; a piece past the
+// row has from = 8.  So every load is one wide access and none sits behind a branch.
+// L > 0: short rows, L lanes of a wave each, 256 / L rows a workgroup, no barrier.
+template <bool XBF, bool YBF, bool AL, int NJ, int MAXT, int L>
+__global__ __launch_bounds__(MAXT) void block_norm_kernel(NormArgs a) {
   __shared__ float red[3][16];
-  const int64_t m = blockIdx.x;
+  const int64_t m = L ? (int64_t)blockIdx.x * (256 / (L ? L : 1)) + threadIdx.x / (L ? L : 1) : blockIdx.x;
+  if (L && m >= a.M) return;
+  const int tid = L ? threadIdx.x % (L ? L : 1) : threadIdx.x, nthr = L ? L : blockDim.x;
   const uint8_t* xr = a.x + m * a.ldx_b;
   const float invk = 1.0f / (float)a.K;
-  float r[NJ][E], t[NJ][E], g[NJ][E];
-  bool in[NJ];
+  float r[NJ][8], t[NJ][8], g[NJ][8];
+  int col[NJ], from[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int64_t k = (int64_t)E * (threadIdx.x + (int64_t)blockDim.x * j);
-    in[j] = k < a.K;
-    const int64_t ks = in[j] ? k : 0;  // pieces past the row read its first one and are masked
-    load_vals<XBF, E>(r[j], xr, ks);
-    if (a.y) load_vals<YBF, E>(t[j], a.y + m * a.ldy_b, ks);
-    if (a.gate) load_vals<YBF, E>(g[j], a.gate + m * a.ldg_b, ks);
+    const int k = 8 * (tid + nthr * j), last = (int)a.K - 8;
+    col[j] = min(k, last);
+    from[j] = AL ? (k < (int)a.K ? 0 : 8) : min(k - col[j], 8);  // AL: K is a multiple of 8
+    load8<XBF, AL>(r[j], xr, col[j]);
+    if (a.y) load8<YBF, AL>(t[j], a.y + m * a.ldy_b, col[j]);
+    if (a.gate) load8<YBF, AL>(g[j], a.gate + m * a.ldg_b, col[j]);
   }
+  auto squares = [&](const float (&v)[8], int f) {  // of the piece's own elements
+    float ss = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += AL || e >= f ? v[e] * v[e] : 0.0f;
+    return AL && f ? 0.0f : ss;
+  };
   if (a.y) {
     if (a.wpost) {
       float ss = 0.0f;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int e = 0; e < E; ++e) ss += in[j] ? t[j][e] * t[j][e] : 0.0f;
-      const float inv = rsqrtf(block_reduce<false>(ss, red[0]) * invk + a.eps);
+      for (int j = 0; j < NJ; ++j) ss += squares(t[j], from[j]);
+      const float inv = rsqrtf(row_reduce<false, L>(ss, red[0]) * invk + a.eps);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        float w[E];
-        load_weights<E>(w, a.wpost, a.w_bf16, in[j] ? (int64_t)E * (threadIdx.x + (int64_t)blockDim.x * j) : 0);
+        float w[8];
+        weights8<AL>(w, a.wpost, a.w_bf16, col[j]);
 #pragma unroll
-        for (int e = 0; e < E; ++e) t[j][e] = t[j][e] * inv * w[e];
+        for (int e = 0; e < 8; ++e) t[j][e] = t[j][e] * inv * w[e];
       }
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int e = 0; e < E; ++e) r[j][e] = a.alpha * r[j][e] + (a.gate ? g[j][e] * t[j][e] : t[j][e]);
+      for (int e = 0; e < 8; ++e) r[j][e] = a.alpha * r[j][e] + (a.gate ? g[j][e] * t[j][e] : t[j][e]);
   }
   if (a.r) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
-      if (in[j]) store_vals<XBF, E>(r[j], a.r + m * a.ldr_b, (int64_t)E * (threadIdx.x + (int64_t)blockDim.x * j));
+    for (int j = 0; j < NJ; ++j) store8<XBF, AL>(r[j], a.r + m * a.ldr_b, col[j], from[j]);
   }
   if (!a.n && !a.q) return;
   float ss = 0.0f;
 #pragma unroll
-  for (int j = 0; j < NJ; ++j)
-#pragma unroll
-    for (int e = 0; e < E; ++e) ss += in[j] ? r[j][e] * r[j][e] : 0.0f;
-  const float inv = rsqrtf(block_reduce<false>(ss, red[1]) * invk + a.eps);
+  for (int j = 0; j < NJ; ++j) ss += squares(r[j], from[j]);
+  const float inv = rsqrtf(row_reduce<false, L>(ss, red[1]) * invk + a.eps);
   float amax = 0.0f;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int64_t k = (int64_t)E * (threadIdx.x + (int64_t)blockDim.x * j);
-    float w[E];
-    load_weights<E>(w, a.wpre, a.w_bf16, in[j] ? k : 0);
+    float w[8];
+    weights8<AL>(w, a.wpre, a.w_bf16, col[j]);
+    float top = 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < 8; ++e) {
       r[j][e] = r[j][e] * inv * w[e];
-      if (in[j]) amax = fmaxf(amax, fabsf(r[j][e]));
+      if (AL || e >= from[j]) top = fmaxf(top, fabsf(r[j][e]));
     }
-    if (a.n && in[j]) store_vals<YBF, E>(r[j], a.n + m * a.ldn_b, k);
+    if (!AL || !from[j]) amax = fmaxf(amax, top);
+    if (a.n) store8<YBF, AL>(r[j], a.n + m * a.ldn_b, col[j], from[j]);
   }
   if (!a.q) return;
-  amax = block_reduce<true>(amax, red[2]);
+  amax = row_reduce<true, L>(amax, red[2]);
   const float s = amax > 0.0f ? amax / 448.0f : 1.0f;
-  if (threadIdx.x == 0) a.scales[m] = s;
+  if (tid == 0) a.scales[m] = s;
+  const Divisor<NJ == 1> d(s);
 #pragma unroll
-  for (int j = 0; j < NJ; ++j)
-    if (in[j]) store_codes<E>(r[j], s, a.q + m * a.ldq, (int64_t)E * (threadIdx.x + (int64_t)blockDim.x * j));
+  for (int j = 0; j < NJ; ++j) codes8<AL>(r[j], d, a.q + m * a.ldq, col[j], from[j]);
 }
 
 // Rows of any length: four passes over the row (the later ones from L2), each forming the
@@ -225,25 +311,17 @@ __global__ __launch_bounds__(1024) void block_norm_long_kernel(NormArgs a) {
   if (yr && a.wpost) {
     float ss = 0.0f;
     for (int64_t k = threadIdx.x; k < a.K; k += blockDim.x) {
-      float v[1];
-      load_vals<YBF, 1>(v, yr, k);
-      ss += v[0] * v[0];
+      const float v = load1<YBF>(yr, k);
+      ss += v * v;
     }
-    inv1 = rsqrtf(block_reduce<false>(ss, red[0]) * invk + a.eps);
+    inv1 = rsqrtf(row_reduce<false>(ss, red[0]) * invk + a.eps);
   }
   auto residual = [&](int64_t k) {
-    float x[1];
-    load_vals<XBF, 1>(x, xr, k);
-    if (!yr) return x[0];
-    float t[1], w[1], g[1] = {1.0f};
-    load_vals<YBF, 1>(t, yr, k);
-    if (a.wpost) {
-      load_weights<1>(w, a.wpost, a.w_bf16, k);
-      t[0] = t[0] * inv1 * w[0];
-    }
-    if (!a.gate) return a.alpha * x[0] + t[0];
-    load_vals<YBF, 1>(g, a.gate + m * a.ldg_b, k);
-    return a.alpha * x[0] + g[0] * t[0];
+    const float x = load1<XBF>(xr, k);
+    if (!yr) return x;
+    float t = load1<YBF>(yr, k);
+    if (a.wpost) t = t * inv1 * weight1(a.wpost, a.w_bf16, k);
+    return a.alpha * x + (a.gate ? load1<YBF>(a.gate + m * a.ldg_b, k) * t : t);
   };
   float inv = 1.0f, s = 1.0f;
   if (a.n || a.q) {
@@ -252,44 +330,55 @@ __global__ __launch_bounds__(1024) void block_norm_long_kernel(NormArgs a) {
       const float r = residual(k);
       ss += r * r;
     }
-    inv = rsqrtf(block_reduce<false>(ss, red[1]) * invk + a.eps);
+    inv = rsqrtf(row_reduce<false>(ss, red[1]) * invk + a.eps);
   }
-  auto normed = [&](float r, int64_t k) {
-    float w[1];
-    load_weights<1>(w, a.wpre, a.w_bf16, k);
-    return r * inv * w[0];
-  };
+  auto normed = [&](float r, int64_t k) { return r * inv * weight1(a.wpre, a.w_bf16, k); };
   if (a.q) {
     float amax = 0.0f;
     for (int64_t k = threadIdx.x; k < a.K; k += blockDim.x) amax = fmaxf(amax, fabsf(normed(residual(k), k)));
-    amax = block_reduce<true>(amax, red[2]);
+    amax = row_reduce<true>(amax, red[2]);
     s = amax > 0.0f ? amax / 448.0f : 1.0f;
     if (threadIdx.x == 0) a.scales[m] = s;
   }
+  const Divisor<true> d(s);
   for (int64_t k = threadIdx.x; k < a.K; k += blockDim.x) {
-    const float r[1] = {residual(k)};
-    const float n[1] = {normed(r[0], k)};
-    if (a.r) store_vals<XBF, 1>(r, a.r + m * a.ldr_b, k);
-    if (a.n) store_vals<YBF, 1>(n, a.n + m * a.ldn_b, k);
-    if (a.q) store_codes<1>(n, s, a.q + m * a.ldq, k);
+    const float r = residual(k), n = normed(r, k);
+    if (a.r) store1<XBF>(r, a.r + m * a.ldr_b, k);
+    if (a.n) store1<YBF>(n, a.n + m * a.ldn_b, k);
+    if (a.q) a.q[m * a.ldq + k] = code1(n, d);
   }
 }
 
-template <bool XBF, bool YBF>
-hipError_t launch_norm(const NormArgs& a, int64_t M, bool vec, hipStream_t st) {
-  const dim3 grid((unsigned)M);
-  auto launch = [&](auto kernel, int64_t per_thread) {
-    const int64_t threads = ((a.K + per_thread - 1) / per_thread + 63) / 64 * 64;
-    hipLaunchKernelGGL(kernel, grid, dim3((unsigned)threads), 0, st, a);
+constexpr int64_t kManyRows = 512;
+
+template <bool XBF, bool YBF, bool AL>
+hipError_t launch_norm_rows(const NormArgs& a, int64_t M, hipStream_t st) {
+  auto launch = [&](auto kernel, int64_t nj) {
+    const int64_t threads = ((a.K + 8 * nj - 1) / (8 * nj) + 63) / 64 * 64;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)M), dim3((unsigned)threads), 0, st, a);
     return hipGetLastError();
   };
-  if (vec && a.K <= 8192) return launch(block_norm_kernel<XBF, YBF, 8, 1>, 8);
-  if (vec && a.K <= 16384) return launch(block_norm_kernel<XBF, YBF, 8, 2>, 16);
-  if (vec && a.K <= 32768) return launch(block_norm_kernel<XBF, YBF, 8, 4>, 32);
-  if (a.K <= 4096) return launch(block_norm_kernel<XBF, YBF, 1, 4>, 4);
-  if (a.K <= 16384) return launch(block_norm_kernel<XBF, YBF, 1, 16>, 16);
-  hipLaunchKernelGGL((block_norm_long_kernel<XBF, YBF>), grid, dim3(1024), 0, st, a);
-  return hipGetLastError();
+  auto launch_short = [&](auto kernel, int64_t lanes) {
+    const int64_t rows = 256 / lanes;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((M + rows - 1) / rows)), dim3(256), 0, st, a);
+    return hipGetLastError();
+  };
+  if (a.K <= 128) return launch_short(block_norm_kernel<XBF, YBF, AL, 1, 256, 16>, 16);
+  if (a.K <= 256) return launch_short(block_norm_kernel<XBF, YBF, AL, 1, 256, 32>, 32);
+  if (a.K <= 512) return launch_short(block_norm_kernel<XBF, YBF, AL, 1, 256, 64>, 64);
+  if (M >= kManyRows && a.K <= 8192) return launch(block_norm_kernel<XBF, YBF, AL, 2, 512, 0>, 2);
+  if (a.K <= 8192) return launch(block_norm_kernel<XBF, YBF, AL, 1, 1024, 0>, 1);
+  if (a.K <= 16384) return launch(block_norm_kernel<XBF, YBF, AL, 2, 1024, 0>, 2);
+  return launch(block_norm_kernel<XBF, YBF, AL, 4, 1024, 0>, 4);
+}
+
+template <bool XBF, bool YBF>
+hipError_t launch_norm(const NormArgs& a, int64_t M, bool aligned, hipStream_t st) {
+  if (a.K < 8 || a.K > 32768) {
+    hipLaunchKernelGGL((block_norm_long_kernel<XBF, YBF>), dim3((unsigned)M), dim3(1024), 0, st, a);
+    return hipGetLastError();
+  }
+  return aligned ? launch_norm_rows<XBF, YBF, true>(a, M, st) : launch_norm_rows<XBF, YBF, false>(a, M, st);
 }
 
 }  // namespace
@@ -341,7 +430,7 @@ extern "C" int spense_block_norm(const spense_block_norm_t* p, hipStream_t strea
   a.gate = static_cast<const uint8_t*>(b.gate), a.ldg_b = b.ldg * ys;
   a.wpost = static_cast<const uint8_t*>(b.post_weight), a.wpre = static_cast<const uint8_t*>(b.weight);
   a.w_bf16 = b.w_type == SPENSE_BF16;
-  a.alpha = b.residual_scale, a.eps = b.eps, a.K = b.K;
+  a.alpha = b.residual_scale, a.eps = b.eps, a.M = b.M, a.K = b.K;
   a.r = static_cast<uint8_t*>(b.residual), a.ldr_b = b.ldr * xs;
   a.n = static_cast<uint8_t*>(b.normed), a.ldn_b = b.ldn * ys;
   a.q = b.q, a.ldq = b.ldq, a.scales = b.scales;
