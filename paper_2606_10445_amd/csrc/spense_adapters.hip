@@ -36,7 +36,6 @@ struct AdapterArgs {
   float* part;  // slices x M x R
   int32_t M, K, N, R, count, slices;
   uint32_t x_bytes;
-  int32_t vec;       // base and Y rows in aligned pieces of eight
   int32_t in_place;  // base is Y: rows without an adapter are left alone
   int32_t nblocks;   // second launch: workgroups along N
   int32_t steps;     // and steps of 128 columns each of them takes
@@ -157,7 +156,8 @@ __global__ __launch_bounds__(64 * NW) void adapter_shrink_kernel(AdapterArgs a) 
   }
 }
 
-// Eight consecutive bf16 or fp32 values as they lie in memory, and as fp32.
+// Eight consecutive bf16 or fp32 values as they lie in memory, and as fp32.  Wide accesses at the
+// alignment of the elements: a row of base or Y may start anywhere.
 template <bool BF>
 struct Eight {
   v4i d[BF ? 1 : 2];
@@ -167,7 +167,7 @@ template <bool BF>
 __device__ __forceinline__ Eight<BF> load8(const uint8_t* row, int n) {
   Eight<BF> v;
 #pragma unroll
-  for (int h = 0; h < (BF ? 1 : 2); ++h) v.d[h] = *reinterpret_cast<const v4i*>(row + (BF ? 2 : 4) * (int64_t)n + 16 * h);
+  for (int h = 0; h < (BF ? 1 : 2); ++h) v.d[h] = load16u<BF ? 2 : 4>(row + (BF ? 2 : 4) * (int64_t)n + 16 * h);
   return v;
 }
 
@@ -182,14 +182,14 @@ __device__ __forceinline__ float value(const Eight<BF>& v, int e) {
 template <bool BF>
 __device__ __forceinline__ void store8(const float (&v)[8], uint8_t* row, int n) {
   if constexpr (BF) {
-    u4 d;
+    v4i d;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) d[e] = bf16_bits(v[2 * e]) | (bf16_bits(v[2 * e + 1]) << 16);
-    *reinterpret_cast<u4*>(row + 2 * (int64_t)n) = d;
+    for (int e = 0; e < 4; ++e) d[e] = (int)(bf16_bits(v[2 * e]) | (bf16_bits(v[2 * e + 1]) << 16));
+    store16u<2>(row + 2 * (int64_t)n, d);
   } else {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      *reinterpret_cast<v4f*>(row + 4 * (int64_t)n + 16 * h) = (v4f){v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+      store16u<4>(row + 4 * (int64_t)n + 16 * h, __builtin_bit_cast(v4i, (v4f){v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]}));
   }
 }
 
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
     return load8<BBF>(a.base + (int64_t)max(row[c], 0) * a.ldb_b, n_wg + 32 * (4 * s + wave) + 8 * lq);
   };
   // whole pieces of eight for every lane of the step (the same for all of the wave)
-  auto whole = [&](int s) { return a.vec && n_wg + 32 * (4 * s + wave) + 32 <= a.N; };
+  auto whole = [&](int s) { return n_wg + 32 * (4 * s + wave) + 32 <= a.N; };
   Eight<BBF> ob[U][CT];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) o[e] = none ? value<BBF>(ob[u][c], e) : value<BBF>(ob[u][c], e) + acc[c][e / 4][e % 4];
           if (row[c] >= 0) store8<YBF>(o, yr, nq);
-        } else if (row[c] >= 0) {
+        } else if (row[c] >= 0) {  // the ragged end of N
           const uint8_t* br = a.base + (int64_t)row[c] * a.ldb_b;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -456,12 +456,13 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   if (P.K * P.R * 2 >= lim || P.N * P.R * 2 >= lim) return api_fail(SPENSE_ERR_ARG, "an adapter spans 2 GiB or more");
   const int T = spense::expand_tokens(M, P.count, P.R), Ts = spense::shrink_tokens(M, P.count, P.R);
   const int64_t tiles = spense::most_tiles(M, P.count, false, Ts), all_tiles = spense::most_tiles(M, P.count, true, T);
-  // columns a workgroup: 1024 where that leaves workgroups enough, their start (the tile, V) then paid
-  // less often, else 256; 512 in tiles of 64.  us at 256 / 512 / 1024: M = 64 over 28 adapters, N =
+  // columns a workgroup: as many of 1024 (tiles of 16), 512 or 256 as leave workgroups enough, their
+  // start (the tile, V) then paid less often.  us at 256 / 512 / 1024: M = 64 over 28 adapters, N =
   // 25600 18.9 / 17.3 / 15.4; M = 1 7.9 / 8.6 / 10.0, M = 128 over 8, N = 8192 9.6 / 10.3 / 12.6; M =
   // 2048, N = 8192 in tiles of 64 55.6 / 52.3 / 58.9.
-  const int64_t tiles_used = P.count < M ? P.count : M;
-  const int steps = T == 64 ? 4 : tiles_used * ((P.N + 1023) / 1024) >= 512 ? 8 : 2;
+  const int64_t used = P.count < M ? P.count : M, tiles_used = T == 64 ? M / 64 + used / 2 : used;
+  int steps = T == 64 ? 4 : 8;
+  while (steps > 2 && tiles_used * ((P.N + 128 * steps - 1) / (128 * steps)) < 512) steps /= 2;
   const int64_t nblocks = (P.N + 128 * steps - 1) / (128 * steps);
   if (all_tiles * nblocks > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "M x N too large for the grid");
   const size_t need = spense_adapters_workspace_size(M, pool);
@@ -479,7 +480,6 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   a.M = (int32_t)M, a.K = (int32_t)P.K, a.N = (int32_t)P.N, a.R = P.R, a.count = P.count;
   a.slices = spense::k_slices(M, P.count, P.K, P.R);
   a.x_bytes = (uint32_t)xb;
-  a.vec = at(base) % 16 == 0 && a.ldb_b % 16 == 0 && at(Y) % 16 == 0 && a.ldy_b % 16 == 0;
   a.in_place = same;
   a.nblocks = (int32_t)nblocks;
   a.steps = steps;

@@ -396,7 +396,7 @@ int check_call(Call& c, const void* X, int64_t rows_x, int64_t ldx, const float*
 void set_output(Call& c, int i, void* Y, int64_t ldy, bool f32) {
   c.out_f32 = f32;
   c.mat[i].Y = Y, c.mat[i].ldy = ldy;
-  c.mat[i].vec_store = (c.in_split || c.db % 4 == 0) && ldy % 4 == 0 && reinterpret_cast<uintptr_t>(Y) % (f32 ? 16 : 8) == 0;
+  c.mat[i].vec_store = 1;  // at any alignment of the elements
 }
 
 // A launch of the 128 x 128 or, with `big`, the 256 x 256 kernel; pmax: the gate / up pair, the

@@ -408,7 +408,7 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
   if (n_de > 0) run_dense();
   // bf16 output with 16-byte aligned rows leaves through LDS as whole token rows
   // (out_tile_write)
-  const bool via_lds = !GL && !a.out_f32 && ((uintptr_t)MD.Y % 16 == 0) && (MD.ldy % 8 == 0) && (rblk % 8 == 0);
+  const bool via_lds = !GL && (RG || (!a.out_f32 && ((uintptr_t)MD.Y % 16 == 0) && (MD.ldy % 8 == 0) && (rblk % 8 == 0)));
   const int mw = m0 + 16 * NT * wc + li;
   if constexpr (GL) {
     const float* const sg = RG && a.mat[0].sw ? a.mat[0].sw + ex * er.N : a.mat[0].sw;
@@ -469,9 +469,20 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
     return;
   }
   barrier_vm_lgkm0<0>();  // every wave's last operand reads and copies are done
+  if (RG && a.out_f32) {  // fp32: the two token halves of the tile after each other (straight from the
+                          // accumulators: 32 experts' 5120 x 1536, 256 rows each, 139 us)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if ((wc >> 1) == h) out_tile_write_f32<RPW, NT, kB2Rows / 4>(big_lds, acc, es, MD.sw != nullptr, wr, wc & 1, li, lq);
+      barrier_vm_lgkm0<0>();
+      out_tile_store_f32<kB2Rows / 4, 512>(big_lds, 32 * NT, m0 + 32 * NT * h, mend, rblk, rowend, MD.Y, MD.ldy);
+      if (h == 0) barrier_vm_lgkm0<0>();
+    }
+    return;
+  }
   out_tile_write<RPW, NT, kB2Rows / 8>(big_lds, acc, es, MD.sw != nullptr, wr, wc, li, lq);
   barrier_vm_lgkm0<0>();
-  out_tile_store<kB2Rows / 8, 512>(big_lds, ntok, m0, mend, rblk, rowend, MD.Y, MD.ldy);
+  out_tile_store<kB2Rows / 8, 512, !RG>(big_lds, ntok, m0, mend, rblk, rowend, MD.Y, MD.ldy);
   };
   if (ntok > 192)
     tile(std::integral_constant<int, 4>());

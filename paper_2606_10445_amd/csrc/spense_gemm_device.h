@@ -240,13 +240,16 @@ __device__ __forceinline__ uint32_t bf16_bits(float v) {
 
 // Epilogue of 4 consecutive output rows n0.. of token m: (acc * w_scale[n]) * x_scale[m],
 // bf16 (round to nearest even) or fp32, one vector store where allowed.
-// Y[m, n0 + r] = v[r] for r < 4 (rows before rowend), bf16 RNE or fp32 per a.out_f32.
+// Y[m, n0 + r] = v[r] for r < 4 (rows before rowend), bf16 RNE or fp32 per a.out_f32.  vec_store: as one
+// vector store, whose address need be aligned to the elements only (the planner asks for aligned
+// quads; the grouped products do without).
 __device__ __forceinline__ void put4(void* Y, int64_t ldy, int vec_store, const GemmArgs& a, const float (&v)[4], int m,
                                      int n0, int rowend) {
   if (a.out_f32) {
     float* yp = reinterpret_cast<float*>(Y) + (int64_t)m * ldy + n0;
     if (vec_store && n0 + 3 < rowend) {
-      *reinterpret_cast<v4f*>(yp) = (v4f){v[0], v[1], v[2], v[3]};
+      typedef float v4fu __attribute__((ext_vector_type(4), aligned(4)));
+      *reinterpret_cast<v4fu*>(yp) = (v4fu){v[0], v[1], v[2], v[3]};
     } else {
 #pragma unroll
       for (int r = 0; r < 4; ++r)
@@ -256,7 +259,7 @@ __device__ __forceinline__ void put4(void* Y, int64_t ldy, int vec_store, const 
     uint16_t* yp = reinterpret_cast<uint16_t*>(Y) + (int64_t)m * ldy + n0;
     const uint32_t b0 = bf16_bits(v[0]), b1 = bf16_bits(v[1]), b2 = bf16_bits(v[2]), b3 = bf16_bits(v[3]);
     if (vec_store && n0 + 3 < rowend) {
-      typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+      typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
       *reinterpret_cast<u2*>(yp) = (u2){b0 | (b1 << 16), b2 | (b3 << 16)};
     } else {
       const uint32_t bb[4] = {b0, b1, b2, b3};
@@ -353,8 +356,9 @@ __device__ __forceinline__ void out_tile_write(uint8_t* ot, const v4f (&acc)[RT]
 }
 
 // out_tile_store: the tile's first ntok token rows to Y (tile row 0 = output row rblk,
-// token 0 = m0), 16 bytes per thread; Y 16-byte aligned, ldy and rblk multiples of 8.
-template <int NB, int NTHR>
+// token 0 = m0), 16 bytes per thread; Y 16-byte aligned, ldy and rblk multiples of 8 (AL), or
+// anything.
+template <int NB, int NTHR, bool AL = true>
 __device__ __forceinline__ void out_tile_store(const uint8_t* ot, int ntok, int m0, int M, int rblk, int rowend, void* Y,
                                                int64_t ldy) {
   for (int q = threadIdx.x; q < ntok * NB; q += NTHR) {
@@ -364,9 +368,53 @@ __device__ __forceinline__ void out_tile_store(const uint8_t* ot, int ntok, int 
     const v4i d = *reinterpret_cast<const v4i*>(ot + r * (16 * NB) + ((b ^ (r % NB)) << 4));
     uint16_t* yp = reinterpret_cast<uint16_t*>(Y) + (int64_t)m * ldy + n;
     if (n + 8 <= rowend) {
-      *reinterpret_cast<v4i*>(yp) = d;
+      if constexpr (AL) {
+        *reinterpret_cast<v4i*>(yp) = d;
+      } else {
+        typedef int v4iu __attribute__((ext_vector_type(4), aligned(2)));
+        *reinterpret_cast<v4iu*>(yp) = d;
+      }
     } else {
       for (int e = 0; e < rowend - n; ++e) yp[e] = (uint16_t)((uint32_t)d[e >> 1] >> (16 * (e & 1)));
+    }
+  }
+}
+
+// The same for fp32 outputs, NB 16-byte blocks of four outputs a token: the rows of Y
+// need no alignment (a tile of 256 x 256 takes two goes of half the tokens).
+template <int RT, int CT, int NB>
+__device__ __forceinline__ void out_tile_write_f32(uint8_t* ot, const v4f (&acc)[RT][CT], const EpiScales<RT, CT>& es,
+                                                   bool wscaled, int wr, int wc, int li, int lq) {
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      v4f v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float y = acc[t][c][r];
+        if (wscaled) y = y * es.w[t][r];
+        v[r] = y * es.x[c];
+      }
+      const int r = 16 * (CT * wc + c) + li, b = 4 * (RT * wr + t) + lq;
+      *reinterpret_cast<v4f*>(ot + r * (16 * NB) + ((b ^ (r % NB)) << 4)) = v;
+    }
+}
+
+template <int NB, int NTHR>
+__device__ __forceinline__ void out_tile_store_f32(const uint8_t* ot, int ntok, int m0, int M, int rblk, int rowend, void* Y,
+                                                   int64_t ldy) {
+  for (int q = threadIdx.x; q < ntok * NB; q += NTHR) {
+    const int r = q / NB, b = q % NB;
+    const int m = m0 + r, n = rblk + 4 * b;
+    if (m >= M || n >= rowend) continue;
+    const v4f d = *reinterpret_cast<const v4f*>(ot + r * (16 * NB) + ((b ^ (r % NB)) << 4));
+    float* yp = reinterpret_cast<float*>(Y) + (int64_t)m * ldy + n;
+    if (n + 4 <= rowend) {
+      typedef float v4fu __attribute__((ext_vector_type(4), aligned(4)));
+      *reinterpret_cast<v4fu*>(yp) = d;
+    } else {
+      for (int e = 0; e < rowend - n; ++e) yp[e] = d[e];
     }
   }
 }

@@ -322,7 +322,8 @@ __device__ __forceinline__ void mid_body(const GemmArgs& a, const ExpertRows& er
       }
     return;
   }
-  const bool via_lds = !a.out_f32 && ((uintptr_t)MD.Y % 16 == 0) && (MD.ldy % 8 == 0) && (rblk % 8 == 0);
+  // grouped rows: any output through LDS
+  const bool via_lds = RG || (!a.out_f32 && ((uintptr_t)MD.Y % 16 == 0) && (MD.ldy % 8 == 0) && (rblk % 8 == 0));
   EpiScales<RPW, TC> es;
   const float* sw = RG && MD.sw ? MD.sw + ex * er.N : MD.sw;
   if (!idle) {
@@ -341,9 +342,15 @@ __device__ __forceinline__ void mid_body(const GemmArgs& a, const ExpertRows& er
     return;
   }
   barrier_vm_lgkm0<0>();  // every wave's last operand reads and copies are done
+  if (RG && a.out_f32) {
+    if (!idle) out_tile_write_f32<RPW, TC, kMidRows / 4>(mid_lds, acc, es, MD.sw != nullptr, wr, wc, li, lq);
+    barrier_vm_lgkm0<0>();
+    out_tile_store_f32<kMidRows / 4, 768>(mid_lds, kMidTok, m0, mend, rblk, rowend, MD.Y, MD.ldy);
+    return;
+  }
   if (!idle) out_tile_write<RPW, TC, kMidRows / 8>(mid_lds, acc, es, MD.sw != nullptr, wr, wc, li, lq);
   barrier_vm_lgkm0<0>();
-  out_tile_store<kMidRows / 8, 768>(mid_lds, kMidTok, m0, mend, rblk, rowend, MD.Y, MD.ldy);
+  out_tile_store<kMidRows / 8, 768, !RG>(mid_lds, kMidTok, m0, mend, rblk, rowend, MD.Y, MD.ldy);
 }
 
 template <int DT>

@@ -5,6 +5,28 @@
 namespace spense {
 namespace {
 
+// Sixteen bytes at any address that is a multiple of ALIGN (the element's size).
+template <int ALIGN>
+struct Unaligned16;
+template <>
+struct Unaligned16<2> {
+  typedef int type __attribute__((ext_vector_type(4), aligned(2)));
+};
+template <>
+struct Unaligned16<4> {
+  typedef int type __attribute__((ext_vector_type(4), aligned(4)));
+};
+typedef int rows_v4i __attribute__((ext_vector_type(4)));
+
+template <int ALIGN>
+__device__ __forceinline__ rows_v4i load16u(const void* p) {
+  return *reinterpret_cast<const typename Unaligned16<ALIGN>::type*>(p);
+}
+template <int ALIGN>
+__device__ __forceinline__ void store16u(void* p, rows_v4i v) {
+  *reinterpret_cast<typename Unaligned16<ALIGN>::type*>(p) = v;
+}
+
 struct RowTile {
   int group;   // count: the rows of no group
   int p0, p1;  // positions [p0, p1), at most T of them
