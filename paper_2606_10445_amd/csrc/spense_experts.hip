@@ -421,8 +421,7 @@ int launch_tiles(Call& c, bool big, float* pmax, int64_t pmax_ld, hipStream_t st
     blocks += R.nrb;
   }
   g.groups = (int32_t)blocks, g.hg0 = g.groups;
-  c.er.row_blocks = (int32_t)(ceil_div(blocks, 8) * 8);
-  if (spense::most_tiles(c.er.n, c.er.count, false, big ? 256 : 128) * c.er.row_blocks > INT32_MAX)
+  if (spense::most_tiles(c.er.n, c.er.count, false, big ? 256 : 128) * blocks > INT32_MAX - 8)
     return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
   int rc = spense::api_check_device();
   if (rc) return rc;

@@ -91,9 +91,7 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
   bool half = false;
   RowTile rt = {0, 0, 0};
   if constexpr (RG) {
-    const int per = er.row_blocks >> 3, x = g & 7, l = g >> 3;
-    g = (l % per) * 8 + x;
-    if (g >= a.groups || !find_tile(er.offsets, er.count, er.n, false, kB2Tokens, l / per, rt)) return;
+    if (!find_pair(er, kB2Tokens, a.groups, rt, g)) return;
     ri = 0;
     for (int i = 1; i < a.nreg; ++i)
       if (g >= a.reg[i].wg0) ri = i;
@@ -419,6 +417,7 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
     epi_scales(eg, sg, RG ? nullptr : a.sx, a.M, nw, mw, rowend);
     epi_scales(eu, su, nullptr, a.M, nw, mw, rowend);
     if constexpr (RG) source_scales<NT>(eg.x, er, a.sx, mw, mend);
+    if constexpr (RG) barrier_vm_lgkm0<0>();  // the stages are free for H
     // the row block's number over both regions: its two slots of the row maxima
     const int slot = 2 * (R.wg0 / a.tblocks + rb) + wr;
 #pragma unroll
@@ -437,13 +436,22 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
           h[r] = glu_silu(gg * eg.x[c], uu * eg.x[c]);
           if (n0 + r < rowend) tmax = fmaxf(tmax, fabsf(h[r]));
         }
-        if (m < mend && n0 < rowend) put4(MD.Y, MD.ldy, MD.vec_store, a, h, m, n0, rowend);
+        if constexpr (RG) {  // as out_tile_write_f32: 128 rows are 32 blocks a token
+          const int r = 16 * (NT * wc + c) + li, b = 16 * wr + 4 * t + lq;
+          *reinterpret_cast<v4f*>(big_lds + r * 512 + ((b ^ (r % 32)) << 4)) = (v4f){h[0], h[1], h[2], h[3]};
+        } else {
+          if (m < a.M && n0 < rowend) put4(MD.Y, MD.ldy, MD.vec_store, a, h, m, n0, rowend);
+        }
       }
       if (a.hmax) {
         tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
         tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
         if (lq == 0 && m < mend) a.hmax[(int64_t)m * a.hmax_ld + slot] = tmax;
       }
+    }
+    if constexpr (RG) {
+      barrier_vm_lgkm0<0>();
+      out_tile_store_f32<32, 512>(big_lds, 64 * NT, m0, mend, rblk, rowend, MD.Y, MD.ldy);
     }
     return;
   }
@@ -527,7 +535,7 @@ hipError_t launch_experts_big2(const GemmArgs& a, const ExpertRows& er, hipStrea
   auto k = glu ? spense_experts_big2_kernel<kB2Glu> : spense_experts_big2_kernel<kB2Grouped>;
   hipError_t e = set_big_lds(k, 0, glu ? 1 : 0, kB2Lds);
   if (e != hipSuccess) return e;
-  const int64_t grid = most_tiles(er.n, er.count, false, kB2Tokens) * er.row_blocks;
+  const int64_t grid = (most_tiles(er.n, er.count, false, kB2Tokens) * a.groups + 7) / 8 * 8;
   hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(512), kB2Lds, s, a, er);
   return hipGetLastError();
 }

@@ -39,10 +39,8 @@ constexpr int kMidRows = 128, kMidTok = 128, kMidX = kMidTok * 128, kMidStage = 
 constexpr int kMidStages = 5, kMidLds = kMidStages * kMidStage;
 
 // RG: rows grouped by expert.  A workgroup's tokens are a tile of positions of one expert
-// (find_tile; positions past the last tile's end have no workgroup), its weight that expert's
-// (the experts' buffers one after the other), position p reads activation row order[p] / top and
-// writes output row p.  Workgroup 8 l + x takes row blocks x, x + 8, ... of one tile after the
-// other, so that a row block of an expert is read by one XCD only.
+// (find_pair gives the tile and the row block), its weight that expert's (the experts' buffers
+// one after the other), position p reads activation row order[p] / top and writes output row p.
 template <int DT, bool RG>
 __device__ __forceinline__ void mid_body(const GemmArgs& a, const ExpertRows& er) {
   constexpr bool TL = DT == kFP8;  // tiled weights; bf16 reads the row-major layout
@@ -58,9 +56,7 @@ __device__ __forceinline__ void mid_body(const GemmArgs& a, const ExpertRows& er
   int g = blockIdx.x;
   RowTile rt = {0, 0, 0};
   if constexpr (RG) {
-    const int per = er.row_blocks >> 3, x = g & 7, l = g >> 3;
-    g = (l % per) * 8 + x;
-    if (g >= a.groups || !find_tile(er.offsets, er.count, er.n, false, kMidTok, l / per, rt)) return;
+    if (!find_pair(er, kMidTok, a.groups, rt, g)) return;
   } else if (a.xgt > 0 && g < a.xg1) {  // XCD-aware order, as in the 256 x 256 kernel
     const int T = a.tblocks, GT = a.xgt, RC = a.xrc, TGc = T / GT;
     const int x = g & 7, l = g >> 3, tg = x % TGc, rc = x / TGc;
@@ -379,7 +375,7 @@ hipError_t launch_mid(int dtype, const GemmArgs& a, hipStream_t s) {
 hipError_t launch_experts_mid(const GemmArgs& a, const ExpertRows& er, hipStream_t s) {
   hipError_t e = set_big_lds(spense_experts_mid_kernel, 1, 2, kMidLds);
   if (e != hipSuccess) return e;
-  const int64_t grid = most_tiles(er.n, er.count, false, kMidTok) * er.row_blocks;
+  const int64_t grid = (most_tiles(er.n, er.count, false, kMidTok) * a.groups + 7) / 8 * 8;
   hipLaunchKernelGGL(spense_experts_mid_kernel, dim3((unsigned)grid), dim3(768), kMidLds, s, a, er);
   return hipGetLastError();
 }

@@ -110,7 +110,6 @@ struct ExpertRows {
   int32_t top;         // activation row = order[p] / top
   int32_t rows_x;      // activation rows
   int32_t N;           // rows of an expert's weight: the distance of the experts' scales
-  int32_t row_blocks;  // workgroups of a tile of positions
 };
 
 struct LaunchShape {

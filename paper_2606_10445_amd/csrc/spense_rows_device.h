@@ -32,61 +32,90 @@ struct RowTile {
   int p0, p1;  // positions [p0, p1), at most T of them
 };
 
-// Tile g of the tiles of T positions that the groups are cut into, group by group (with
-// `rest`, then those of the positions in no group); false past the last one.  A tile never
-// spans two groups.  The whole wave calls it with the same arguments; each lane counts a
-// contiguous share of the groups, so the search costs one load latency and a prefix over the
-// lanes.  Offsets are clamped to [0, n] and to ascend, so a tile lies in [0, n) whatever they hold.
-__device__ __forceinline__ bool find_tile(const int32_t* __restrict__ offsets, int count, int n, bool rest, int T, int g,
-                                          RowTile& out) {
-  const int lane = threadIdx.x & 63;
-  const int groups = rest ? count + 1 : count;
-  const int per = (groups + 63) >> 6;
-  auto segment = [&](int e, int& a, int& b) {
+// The tiles of T positions that the groups are cut into, group by group (with `rest`, then those of
+// the positions in no group); a tile never spans two groups.  The whole wave makes it with the same
+// arguments; each lane counts a contiguous share of the groups, so the search costs one load latency and
+// a prefix over the lanes.  Offsets are clamped to [0, n] and to ascend, so a tile lies in [0, n)
+// whatever they hold.
+struct RowTiles {
+  const int32_t* offsets;
+  int count, n, groups, per, T;
+  int a0, b0, sum, inc;  // the lane's first group, the tiles of its groups, those up to its last
+  int total;             // all tiles
+
+  __device__ __forceinline__ int tiles_of(int a, int b) const { return (b - a + T - 1) / T; }
+  __device__ __forceinline__ void segment(int e, int& a, int& b) const {
     a = min(max(offsets[e], 0), n);
     b = e < count ? max(min(max(offsets[e + 1], 0), n), a) : n;
-  };
-  int a0 = 0, b0 = 0, sum = 0;  // the lane's first group; its tiles
-  if (lane * per < groups) segment(lane * per, a0, b0);
-  sum = (b0 - a0 + T - 1) / T;
-  const int first = sum;
-  for (int i = 1; i < per; ++i) {
-    const int e = lane * per + i;
-    if (e < groups) {
-      int a, b;
-      segment(e, a, b);
-      sum += (b - a + T - 1) / T;
-    }
   }
-  int inc = sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(inc, o, 64);
-    if (lane >= o) inc += u;
-  }
-  const uint64_t mine = __ballot(g >= inc - sum && g < inc);
-  if (!mine) return false;
-  int at = g - (inc - sum), e = lane * per, p0 = a0 + at * T, p1 = min(b0, p0 + T);
-  bool found = at < first;
-  at -= first;
-  for (int i = 1; i < per; ++i) {
-    const int f = lane * per + i;
-    if (f < groups && !found) {
-      int a, b;
-      segment(f, a, b);
-      const int tiles = (b - a + T - 1) / T;
-      if (at < tiles) {
-        e = f, p0 = a + at * T, p1 = min(b, p0 + T);
-        found = true;
+
+  __device__ __forceinline__ RowTiles(const int32_t* offsets_, int count_, int n_, bool rest, int T_)
+      : offsets(offsets_), count(count_), n(n_), groups(rest ? count_ + 1 : count_), per((groups + 63) >> 6), T(T_), a0(0), b0(0) {
+    const int lane = threadIdx.x & 63;
+    if (lane * per < groups) segment(lane * per, a0, b0);
+    sum = tiles_of(a0, b0);
+    for (int i = 1; i < per; ++i) {
+      const int e = lane * per + i;
+      if (e < groups) {
+        int a, b;
+        segment(e, a, b);
+        sum += tiles_of(a, b);
       }
-      at -= tiles;
     }
+    inc = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(inc, o, 64);
+      if (lane >= o) inc += u;
+    }
+    total = __builtin_amdgcn_readlane(inc, 63);
   }
-  const int src = __builtin_ctzll(mine);
-  out.group = __builtin_amdgcn_readlane(e, src);
-  out.p0 = __builtin_amdgcn_readlane(p0, src);
-  out.p1 = __builtin_amdgcn_readlane(p1, src);
-  return true;
+
+  // Tile g; false past the last one.
+  __device__ __forceinline__ bool find(int g, RowTile& out) const {
+    if (g >= total) return false;
+    const int lane = threadIdx.x & 63;
+    const uint64_t mine = __ballot(g >= inc - sum && g < inc);
+    int at = g - (inc - sum), e = lane * per, p0 = a0 + at * T, p1 = min(b0, p0 + T);
+    bool found = at < tiles_of(a0, b0);
+    at -= tiles_of(a0, b0);
+    for (int i = 1; i < per; ++i) {
+      const int f = lane * per + i;
+      if (f < groups && !found) {
+        int a, b;
+        segment(f, a, b);
+        const int tiles = tiles_of(a, b);
+        if (at < tiles) {
+          e = f, p0 = a + at * T, p1 = min(b, p0 + T);
+          found = true;
+        }
+        at -= tiles;
+      }
+    }
+    const int src = __builtin_ctzll(mine);
+    out.group = __builtin_amdgcn_readlane(e, src);
+    out.p0 = __builtin_amdgcn_readlane(p0, src);
+    out.p1 = __builtin_amdgcn_readlane(p1, src);
+    return true;
+  }
+};
+
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int n, bool rest, int T, int g, RowTile& out) {
+  return RowTiles(offsets, count, n, rest, T).find(g, out);
+}
+
+// Tile and row block of workgroup g of a grid of tiles x row blocks: the pairs, tile by tile, in eight
+// equal runs, one an XCD (workgroup g is on XCD g % 8), so that a tile's activations and an expert's
+// weights are read by one or two XCDs and each has the same number of pairs.  (Row blocks x, x + 8, ... of
+// every tile on XCD x read the weights once too, but 10 row blocks left six XCDs half idle: 32 experts'
+// gate / up of 1536 rows, 256 rows each, 200 us.)
+__device__ __forceinline__ bool find_pair(const ExpertRows& er, int T, int blocks, RowTile& out, int& block) {
+  const RowTiles tiles(er.offsets, er.count, er.n, false, T);
+  const int64_t pairs = (int64_t)tiles.total * blocks, run = (pairs + 7) / 8;
+  const int64_t l = blockIdx.x >> 3, g = (blockIdx.x & 7) * run + l;
+  if (l >= run || g >= pairs) return false;
+  block = (int)(g % blocks);
+  return tiles.find((int)(g / blocks), out);
 }
 
 // The activation row of position p < n, -1 where order names none.
