@@ -294,26 +294,34 @@ enum Kernel { kRows16, kRows32, kRows64, kMid, kBig };
 // against 10.5; 4096 x 2560 22.3 against 23.9; 5120 x 1536 39 against 48).
 constexpr int64_t kStreamChunks = 6;
 
-// Average rows of an expert from which its tiles are computed 256 x 256 (below: 128 x 128).
-constexpr int64_t kBigRows = 96;
+int64_t stream_lds(int64_t chunks, int ct) { return chunks * ct * 8192 + 8 * 16 * spense::kStreamTiles * 4; }
+bool streams(int64_t chunks, int ct) { return chunks <= kStreamChunks && stream_lds(chunks, ct) <= 160 * 1024; }
 
 int64_t rows_per_expert(int64_t n, int64_t count) { return n / (count < n ? count : n); }
+
+// Tiles of 256 x 256 rather than 128 x 128: for many rows an expert where the smaller tiles need a
+// second round of the 256 CUs.  us at 64 / 96 / 112 / 128 / 256 / 512 rows an expert, 128 x 128 and 256 x
+// 256: 32 experts of 1536 x 5120 50 / 54 / 58 / 81 / 117 / 205, 50 / 51 / 52 / 53 / 99 / 142; 32 of 5120 x
+// 1536 60 / 67 / 76 / 97 / 157 / 279, 64 / 66 / 67 / 70 / 104 / 179; 10 of 2915 x 2176 (230 of the smaller
+// tiles up to 128 rows) 16 / 17 / 18 / 30 / 44 / 72, 21 / 22 / 24 / 25 / 31 / 54.
+bool big_tiles(int64_t n, int64_t count, int64_t N, int weights) {
+  const int64_t avg = rows_per_expert(n, count), used = count < n ? count : n;
+  return avg >= 96 && used * ceil_div(avg, 128) * ceil_div(N, 128) * weights > 256;
+}
 
 // The kernel for n rows in count groups: by the rows an expert gets on average where they spread
 // evenly (the counts themselves are on the device).  A tile that an expert's rows do not fit costs its
 // weights again, a wider one little, and less with the activations in LDS.  us at 8 / 12 / 20 / 32 /
 // 40 rows an expert, tiles of 16, 32, 64: 32 experts of 5120 x 1536 39 / 58 / 61 / 81 / 102, 41 / 41
-// / 43 / 67 / 71, 42 / 43 / 44 / 48 / 50; 32 of 1536 x 5120 at 12 / 16 / 24 / 32 36 / - / - / -, 40 /
-// 41 / 45 / 64, 43 / 44 / 47 / 49.  Then 48 / 64 / 96 / 128 / 192, tiles of 64, 128 x 128 and 256 x 256:
-// 1536 x 5120 53 / 74 / 86, 55 / 58 / 65 / 100 / 124, 53 / 53 / 57 / 66 / 81; 5120 x 1536 65 / 76 / -,
-// 59 / 62 / 70 / 93 / 119, 66 / 66 / 69 / 74 / 87; 64 experts of 768 x 2048 30 / 42 / 51, 34 / 36 / 52 /
-// 53 / 77, 43 / 46 / 50 / 53 / 63.
-Kernel choose_kernel(int64_t n, int64_t count, int64_t chunks) {
+// / 43 / 67 / 71, 42 / 43 / 44 / 48 / 50 (128 x 128: 53 at 32, 55 at 48 against 51); 32 of 1536 x 5120 at
+// 12 / 16 / 24 / 32 / 48 36 / - / - / - / -, 40 / 41 / 45 / 64 / 77, 43 / 44 / 47 / 48 / 51, 128 x 128 - /
+// - / 45 / 46 / 46.
+Kernel choose_kernel(int64_t n, int64_t count, int64_t N, int weights, int64_t chunks) {
   const int64_t avg = rows_per_expert(n, count);
-  if (avg >= kBigRows) return kBig;
-  if (avg >= 48) return kMid;
-  const bool stream = chunks <= kStreamChunks;
-  return avg <= (stream ? 8 : 12) ? kRows16 : avg <= (stream ? 18 : 24) ? kRows32 : kRows64;
+  if (big_tiles(n, count, N, weights)) return kBig;
+  if (avg <= (streams(chunks, 1) ? 8 : 12)) return kRows16;
+  if (avg <= (streams(chunks, 2) ? 18 : 24)) return kRows32;
+  return avg < 48 && streams(chunks, 4) ? kRows64 : kMid;
 }
 
 // One call's checked arguments.
@@ -443,8 +451,8 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
   }
   a.tiles = (int32_t)tiles;
   const int64_t most = spense::most_tiles(c.er.n, c.er.count, false, 16 * ct);
-  const int64_t lds = chunks * ct * 8192 + 8 * 16 * spense::kStreamTiles * 4;
-  const bool stream_kernel = chunks <= kStreamChunks && lds <= 160 * 1024;
+  const int64_t lds = stream_lds(chunks, ct);
+  const bool stream_kernel = streams(chunks, ct);
   const int wv = stream_kernel ? 8 : ct == 1 ? 4 : 8;
   if (stream_kernel) {
     auto wgs = [&](int64_t per) {
@@ -476,14 +484,13 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
                                         : ct == 2 ? spense::launch_stream<2>(a, c.er, grid, (int)lds, stream)
                                                   : spense::launch_stream<4>(a, c.er, grid, (int)lds, stream))
                                      : (ct == 1   ? spense::launch_rows<1, 4>(a, c.er, grid, stream)
-                                        : ct == 2 ? spense::launch_rows<2, 8>(a, c.er, grid, stream)
-                                                  : spense::launch_rows<4, 8>(a, c.er, grid, stream));
+                                                  : spense::launch_rows<2, 8>(a, c.er, grid, stream));
   return e == hipSuccess ? SPENSE_OK : api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));
 }
 
 int launch_products(Call& c, hipStream_t stream) {
   const int64_t kbound = c.in_split ? c.db : 0, chunks = ceil_div(kbound, 512) + ceil_div(c.K - kbound, 512);
-  const Kernel k = choose_kernel(c.er.n, c.er.count, chunks);
+  const Kernel k = choose_kernel(c.er.n, c.er.count, c.N, c.weights, chunks);
   if (k >= kMid) return launch_tiles(c, k == kBig, nullptr, 0, stream);
   return launch_few(c, chunks, k == kRows16 ? 1 : k == kRows32 ? 2 : 4, stream);
 }
@@ -522,7 +529,7 @@ int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float*
 
 size_t spense_gemm_experts_glu_fp8_workspace_size(int64_t n, int32_t count, int64_t N) {
   if (n < 1 || n > INT32_MAX || N < 1 || N > INT32_MAX || count < 1 || count > SPENSE_MAX_GROUPS) return 0;
-  if (rows_per_expert(n, count) >= kBigRows) return (size_t)(glu_rows_bytes(n, N) + n * glu_maxima(N) * 4);
+  if (big_tiles(n, count, N, 2)) return (size_t)(glu_rows_bytes(n, N) + n * glu_maxima(N) * 4);
   return (size_t)(2 * glu_rows_bytes(n, N));
 }
 
@@ -548,7 +555,7 @@ int spense_gemm_experts_glu_fp8(const void* X, int64_t rows_x, int64_t ldx, cons
   float* const H = static_cast<float*>(ws);
   float* const second = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + half);
   hipError_t e;
-  if (rows_per_expert(n, count) >= kBigRows) {
+  if (big_tiles(n, count, c.N, 2)) {
     int64_t blocks = 0;
     for (int i = 0; i < c.nreg; ++i)
       if (c.reg[i].mat == 0) blocks += ceil_div(c.reg[i].rows, 128);

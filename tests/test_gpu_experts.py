@@ -97,9 +97,10 @@ def test_experts_exact(S, T, top, E, N, K, split, db, kind):
         assert torch.all(y[n:] == 9)  # rows of no expert
 
 
-LARGE = [  # many rows an expert: tiles of up to 256 positions, of every number of 64-token quarters
-    (450, 1, 2, 300, 352, 0, 112), (700, 2, 3, 513, 544, 1, 288), (1100, 1, 4, 272, 640, 0, 0), (520, 2, 2, 136, 256, 0, 136),
-    (999, 3, 5, 264, 480, 1, 0), (640, 1, 1, 400, 1056, 1, 1056),
+LARGE = [  # many rows an expert: tiles of up to 128 positions, and (from 256 of those on) of 256
+    (450, 1, 2, 300, 352, 0, 112), (520, 2, 2, 136, 256, 0, 136), (640, 1, 1, 400, 1056, 1, 1056), (999, 3, 5, 264, 480, 1, 0),
+    (1040, 1, 8, 2200, 288, 0, 1648), (700, 2, 9, 2065, 352, 1, 160), (530, 2, 11, 2190, 256, 0, 0), (1300, 1, 6, 3200, 320, 1, 320),
+    (2600, 1, 10, 1700, 288, 0, 848),
 ]
 
 
@@ -115,8 +116,8 @@ def test_large_groups_random(S, T, top, E, N, K, split, db):
 
 
 @pytest.mark.parametrize("T,top,E,N,K,db", [(1, 4, 8, 96, 256, 64), (40, 2, 5, 130, 512, 96), (90, 2, 4, 160, 320, 160),
-                                            (150, 3, 6, 257, 544, 128), (600, 1, 2, 300, 352, 112), (900, 2, 3, 513, 512, 0),
-                                            (700, 2, 4, 136, 416, 136)])
+                                            (150, 3, 6, 257, 544, 128), (600, 1, 2, 300, 352, 112), (1040, 1, 8, 1101, 288, 624),
+                                            (700, 2, 9, 1100, 352, 0), (2600, 1, 10, 700, 256, 700)])
 @pytest.mark.parametrize("kind", ["even", "skewed"])
 def test_glu_pair(S, T, top, E, N, K, db, kind):
     """The producer half of the MLP gives the codes and scales of its steps, bit for bit."""
