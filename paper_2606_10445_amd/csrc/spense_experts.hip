@@ -3,11 +3,14 @@
 // and up) in one launch.  Nothing of the grouping is read on the host.
 //
 // Few rows an expert (decoding): the weights of the experts that got rows are the traffic, 0.625
-// byte a 2:4 entry and one a dense entry.  experts_rows_kernel streams them once per tile of 16,
-// 32 or 64 positions: a wave owns 16 weight rows over all of K and keeps two or three chunks of
-// 512 columns in registers ahead of the one in its matrix instructions; the tile's activations,
-// gathered row by row, go through LDS a chunk at a time, shared by the workgroup's waves.
-// Many rows: the 128 x 128 kernel over tiles of positions (spense_gemm_mid.hip).
+// byte a 2:4 entry and one a dense entry.  experts_rows_kernel streams them once per tile of 16 or
+// 32 positions: a wave owns 16 weight rows over all of K and keeps three chunks of 512 columns in
+// registers ahead of the one in its matrix instructions; the tile's activations, gathered row by row,
+// go through LDS a chunk at a time, shared by the workgroup's waves.  64 experts of 1536 x 5120, gate
+// and up, 256 rows: 650 MB of weights in 97 us, 6.7 TB/s.  experts_stream_kernel does the same for a
+// short K, in tiles of up to 64 positions.
+// Many rows: the 128 x 128 and 256 x 256 kernels over tiles of positions (spense_gemm_mid.hip,
+// spense_gemm_big2.hip).
 #include <cstring>
 
 #include "spense_gemm_device.h"
@@ -40,7 +43,7 @@ struct ExpertArgs {
 template <int CT, int WV>
 __global__ __launch_bounds__(64 * WV) void experts_rows_kernel(ExpertArgs a, ExpertRows er) {
   typedef XTile<kFP8, CT> XT;
-  constexpr int NS = CT <= 2 ? 4 : 3, D = NS - 1, P = CT == 1 ? 4 : 1;
+  constexpr int NS = 4, D = NS - 1, P = CT == 1 ? 4 : 1;
   constexpr int KC = XT::CHUNK_K, XI = XT::BYTES / 1024 / WV, NL = 9;  // loads a chunk: activations, weights
   static_assert(XI >= 1 && XI * 1024 * WV == XT::BYTES, "an activation chunk splits evenly over the waves");
   RowTile t;
@@ -141,18 +144,19 @@ __global__ __launch_bounds__(64 * WV) void experts_rows_kernel(ExpertArgs a, Exp
 }
 
 // Where a tile's activations fit LDS whole (16 CT rows x K): copied once behind one barrier, after
-// which each wave streams the weights of its row tiles (`tiles_wave` of them, eight apart) on its
+// which each wave streams the weights of its row tiles (`tiles_wave` of them, WV apart) on its
 // own, the next tile's first chunks requested while the last of this one are multiplied.  The start
-// of a workgroup (finding its tile, the activations) is then paid once per eight times tiles_wave row
+// of a workgroup (finding its tile, the activations) is then paid once per WV times tiles_wave row
 // tiles, and a short K does not drain the pipeline between them.  A workgroup's row tiles are of one
-// region.
+// region.  Tiles of 16 positions: workgroups of four waves, three of them a CU (8 experts of 5120 x 1536,
+// 4 rows each: 11.8 us against 13.9 with eight waves of four register slots); wider tiles: one of eight.
 constexpr int kStreamTiles = 8;  // most row tiles of a wave
 
-template <int CT>
-__global__ __launch_bounds__(512) void experts_stream_kernel(ExpertArgs a, ExpertRows er) {
+template <int CT, int WV>
+__global__ __launch_bounds__(64 * WV) void experts_stream_kernel(ExpertArgs a, ExpertRows er) {
   typedef XTile<kFP8, CT> XT;
-  constexpr int NS = CT <= 2 ? 4 : 3, D = NS - 1, P = CT == 1 ? 4 : 1;
-  constexpr int KC = XT::CHUNK_K, NL = 9;
+  constexpr int NS = CT == 2 ? 4 : 3, D = NS - 1, P = 1;  // one token tile: three waves a SIMD
+  constexpr int KC = XT::CHUNK_K, XI = XT::BYTES / 1024 / WV, NL = 9;
   RowTile t;
   if (!find_tile(er.offsets, er.count, er.n, false, 16 * CT, blockIdx.x / a.wgs, t)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, li = lane & 15, lq = lane >> 4;
@@ -163,8 +167,8 @@ __global__ __launch_bounds__(512) void experts_stream_kernel(ExpertArgs a, Exper
   const ExpertRegion& R = a.reg[ri];
   const MatDesc& MD = a.mat[R.mat];
   const int64_t e = t.group;
-  const int tiles = (R.rows + 15) / 16, first = (wg - R.wg0) * 8 * a.tiles_wave + wave;  // the wave's row tiles: first, first + 8, ...
-  const int mine = min(a.tiles_wave, (tiles - first + 7) / 8);
+  const int tiles = (R.rows + 15) / 16, first = (wg - R.wg0) * WV * a.tiles_wave + wave;  // the wave's row tiles: first, first + WV, ...
+  const int mine = min(a.tiles_wave, (tiles - first + WV - 1) / WV);
   const int nb = (a.kbound + KC - 1) / KC, chunks = nb + (a.K - a.kbound + KC - 1) / KC;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   float* const lsw = reinterpret_cast<float*>(lds + chunks * XT::BYTES) + wave * (16 * kStreamTiles);  // scales of the wave's rows
@@ -172,11 +176,11 @@ __global__ __launch_bounds__(512) void experts_stream_kernel(ExpertArgs a, Exper
                                rm = rsrc(reinterpret_cast<const uint8_t*>(MD.meta) + e * MD.m_bytes, MD.m_bytes),
                                rd = rsrc(MD.dense + e * MD.d_bytes, MD.d_bytes),
                                rs = rsrc(MD.sw ? MD.sw + e * er.N : nullptr, MD.sw ? 4u * (uint32_t)er.N : 0u);
-  uint32_t xo[CT];
-  int col[CT];
+  uint32_t xo[XI];
+  int col[XI];
 #pragma unroll
-  for (int i = 0; i < CT; ++i) {
-    const int byte = (wave * CT + i) * 1024 + 16 * lane, r = byte / XT::ROW_B;
+  for (int i = 0; i < XI; ++i) {
+    const int byte = (wave * XI + i) * 1024 + 16 * lane, r = byte / XT::ROW_B;
     col[i] = 16 * (((byte % XT::ROW_B) >> 4) ^ (r & 31));
     const int src = t.p0 + r < t.p1 ? source_row(er, t.p0 + r) : -1;
     xo[i] = src >= 0 ? (uint32_t)((int64_t)src * a.ldx_b) + (uint32_t)col[i] : kOOB;
@@ -186,14 +190,14 @@ __global__ __launch_bounds__(512) void experts_stream_kernel(ExpertArgs a, Exper
   // scales, four row tiles a load: lane l row l % 16 of row tile l / 16
 #pragma unroll
   for (int i = 0; i < kStreamTiles / 4; ++i) {
-    const int srow = 16 * (first + 8 * (4 * i + lq)) + li;
+    const int srow = 16 * (first + WV * (4 * i + lq)) + li;
     lds_load4<0>(rs, reinterpret_cast<uint8_t*>(lsw + 64 * i), srow < R.rows ? 4u * (uint32_t)(R.row0 + srow) : kOOB, 0);
   }
   for (int c = 0; c < chunks; ++c) {
     const int kc = c < nb ? c * KC : a.kbound + (c - nb) * KC, ke = c < nb ? a.kbound : a.K;
 #pragma unroll
-    for (int i = 0; i < CT; ++i)
-      lds_load16<0>(rx, lds + c * XT::BYTES + (wave * CT + i) * 1024, kc + col[i] < ke ? xo[i] : kOOB, kc);
+    for (int i = 0; i < XI; ++i)
+      lds_load16<0>(rx, lds + c * XT::BYTES + (wave * XI + i) * 1024, kc + col[i] < ke ? xo[i] : kOOB, kc);
   }
   auto run = [&](auto act_const) {
     constexpr bool ACT = decltype(act_const)::value;
@@ -207,9 +211,9 @@ __global__ __launch_bounds__(512) void experts_stream_kernel(ExpertArgs a, Exper
       --left;
       if (++lc == chunks) {
         lc = 0;
-        vt += 8u * (uint32_t)R.n_sp * 4096u;
-        mt += 8u * (uint32_t)R.n_sp * 1024u;
-        dt += 8u * (uint32_t)R.n_de * 8192u;
+        vt += (uint32_t)WV * (uint32_t)R.n_sp * 4096u;
+        mt += (uint32_t)WV * (uint32_t)R.n_sp * 1024u;
+        dt += (uint32_t)WV * (uint32_t)R.n_de * 8192u;
       }
     };
     if constexpr (ACT) {
@@ -233,7 +237,7 @@ __global__ __launch_bounds__(512) void experts_stream_kernel(ExpertArgs a, Exper
         __builtin_amdgcn_sched_barrier(0);
         if (++cc == chunks) {
           xdl_fence();
-          const int n0 = R.row0 + 16 * (first + 8 * r) + 4 * lq, rowend = R.row0 + R.rows;
+          const int n0 = R.row0 + 16 * (first + WV * r) + 4 * lq, rowend = R.row0 + R.rows;
           const v4f w = MD.sw ? *reinterpret_cast<const v4f*>(lsw + 16 * r + 4 * lq) : (v4f){1.f, 1.f, 1.f, 1.f};
           GemmArgs o;
           o.out_f32 = a.out_f32;
@@ -269,11 +273,11 @@ hipError_t launch_rows(const ExpertArgs& a, const ExpertRows& er, int64_t grid, 
   return hipGetLastError();
 }
 
-template <int CT>
+template <int CT, int WV>
 hipError_t launch_stream(const ExpertArgs& a, const ExpertRows& er, int64_t grid, int lds, hipStream_t s) {
-  const hipError_t e = set_big_lds(experts_stream_kernel<CT>, 0, CT, 160 * 1024);
+  const hipError_t e = set_big_lds(experts_stream_kernel<CT, WV>, 0, CT, 160 * 1024);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(experts_stream_kernel<CT>, dim3((unsigned)grid), dim3(512), lds, s, a, er);
+  hipLaunchKernelGGL((experts_stream_kernel<CT, WV>), dim3((unsigned)grid), dim3(64 * WV), lds, s, a, er);
   return hipGetLastError();
 }
 
@@ -453,23 +457,23 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
   const int64_t most = spense::most_tiles(c.er.n, c.er.count, false, 16 * ct);
   const int64_t lds = stream_lds(chunks, ct);
   const bool stream_kernel = streams(chunks, ct);
-  const int wv = stream_kernel ? 8 : ct == 1 ? 4 : 8;
+  const int wv = ct == 1 ? 4 : 8;
   if (stream_kernel) {
     auto wgs = [&](int64_t per) {
       int64_t w = 0;
       for (int i = 0; i < c.nreg; ++i) {
         a.reg[i].wg0 = (int32_t)w;
-        w += ceil_div(ceil_div(c.reg[i].rows, 16), 8 * per);
+        w += ceil_div(ceil_div(c.reg[i].rows, 16), wv * per);
       }
       return w;
     };
-    // row tiles of a wave: rounds of the 256 CUs (one workgroup each) times a workgroup's time, its
-    // start as long as 90 KB of weights; tiles as even groups would give
+    // row tiles of a wave: rounds of the workgroups that run at once (three of four waves or one of eight a
+    // CU) times a workgroup's time, its start as long as 90 KB of a CU's weights; tiles as even groups give
     const int64_t used = c.er.count < c.er.n ? c.er.count : c.er.n, tiles_even = used * ceil_div(c.er.n / used, 16 * ct);
-    const int64_t step = 128 * c.K * 23 / 32;  // bytes of eight row tiles, a quarter of them dense
+    const int64_t at_once = 256 * (ct == 1 ? 3 : 1), step = (ct == 1 ? 192 : 128) * c.K * 23 / 32;  // a CU's bytes for one row tile a wave, a quarter of them dense
     int64_t best = 0;
     for (int64_t per = 1; per <= spense::kStreamTiles; ++per) {
-      const int64_t cost = ceil_div(tiles_even * wgs(per), 256) * (90000 + per * step);
+      const int64_t cost = ceil_div(tiles_even * wgs(per), at_once) * (90000 + per * step);
       if (per == 1 || cost < best) best = cost, a.tiles_wave = (int32_t)per;
     }
     a.wgs = (int32_t)wgs(a.tiles_wave);
@@ -480,9 +484,9 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
   if (grid > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
   int rc = spense::api_check_device();
   if (rc) return rc;
-  const hipError_t e = stream_kernel ? (ct == 1   ? spense::launch_stream<1>(a, c.er, grid, (int)lds, stream)
-                                        : ct == 2 ? spense::launch_stream<2>(a, c.er, grid, (int)lds, stream)
-                                                  : spense::launch_stream<4>(a, c.er, grid, (int)lds, stream))
+  const hipError_t e = stream_kernel ? (ct == 1   ? spense::launch_stream<1, 4>(a, c.er, grid, (int)lds, stream)
+                                        : ct == 2 ? spense::launch_stream<2, 8>(a, c.er, grid, (int)lds, stream)
+                                                  : spense::launch_stream<4, 8>(a, c.er, grid, (int)lds, stream))
                                      : (ct == 1   ? spense::launch_rows<1, 4>(a, c.er, grid, stream)
                                                   : spense::launch_rows<2, 8>(a, c.er, grid, stream));
   return e == hipSuccess ? SPENSE_OK : api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));

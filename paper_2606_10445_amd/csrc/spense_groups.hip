@@ -1,7 +1,7 @@
 // Rows grouped by an index (expert or adapter), and the rows of a token's experts summed back.
 //
 // Grouping is a stable counting sort in one launch whose workgroups do not wait for each other: a
-// workgroup places 1024 consecutive entries, one a thread, and counts the keys of all n for itself
+// workgroup places 1024 (256) consecutive entries, one a thread, and counts the keys of all n for itself
 // (those before its entries and those after, with LDS additions: whole numbers, the same in any
 // order).  Inside a wave a lane finds the lanes with its key by ballots over the key's bits; its
 // rank is the number of lower ones.  The order is the index order, whatever the timing.
@@ -19,12 +19,12 @@ namespace {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-constexpr int kGroupThreads = 1024, kGroupWaves = kGroupThreads / 64;
-
+template <int kGroupThreads>
 __global__ __launch_bounds__(kGroupThreads) void group_rows_kernel(const int32_t* __restrict__ idx, int64_t n, int groups,
                                                                    int bits, int32_t* __restrict__ order,
                                                                    int32_t* __restrict__ inverse,
                                                                    int32_t* __restrict__ offsets) {
+  constexpr int kGroupWaves = kGroupThreads / 64;
   constexpr int kKeys = SPENSE_MAX_GROUPS + 1;  // the groups and one for entries outside them
   __shared__ int before[kKeys], after[kKeys];   // entries with each key before this workgroup's, and from there on
   __shared__ uint16_t cnt[kGroupWaves][kKeys];  // this workgroup's, by wave
@@ -189,9 +189,12 @@ int spense_group_rows(const int32_t* idx, int64_t n, int32_t groups, int32_t* or
   if (rc) return rc;
   int bits = 1;
   while ((groups >> bits) != 0) ++bits;  // keys 0 .. groups
-  const int64_t blocks = n > 0 ? (n + spense::kGroupThreads - 1) / spense::kGroupThreads : 1;
-  hipLaunchKernelGGL(spense::group_rows_kernel, dim3((unsigned)blocks), dim3(spense::kGroupThreads), 0, stream, idx, n, groups,
-                     bits, order, inverse, offsets);
+  if (n <= 256 && groups < 256)
+    hipLaunchKernelGGL(spense::group_rows_kernel<256>, dim3(1), dim3(256), 0, stream, idx, n, groups, bits, order, inverse,
+                       offsets);
+  else
+    hipLaunchKernelGGL(spense::group_rows_kernel<1024>, dim3((unsigned)((n + 1023) / 1024)), dim3(1024), 0, stream, idx, n,
+                       groups, bits, order, inverse, offsets);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return api_fail(SPENSE_ERR_HIP, "group rows launch failed: %s", hipGetErrorString(e));
   return spense::api_ok();
