@@ -1092,7 +1092,6 @@ def add_adapters(base: torch.Tensor, X: torch.Tensor, pool: AdapterPool, groups:
     groups: group_rows of the tokens' adapter indices over pool.count groups (tokens of no group get
     base).  out may be base."""
     _row_major(X, "X")
-    _row_major(base, "base")
     M = X.shape[0]
     dev = X.device
     xt = SPENSE_BF16 if X.dtype == torch.bfloat16 else _act_code(X)
@@ -1144,6 +1143,7 @@ class PackedExperts:
         L = spense_layout(N, K, SPENSE_FP8_E4M3FN, split, dense_begin)
         self.desc = spense_packed_t(SPENSE_FP8_E4M3FN, split, N, K, dense_begin, _ptr(values), L.values_ld, _ptr(meta),
                                     L.meta_ld, _ptr(dense), L.dense_ld, SPENSE_LAYOUT_TILED)
+        self.desc_array = (ctypes.POINTER(spense_packed_t) * 1)(ctypes.pointer(self.desc))
 
 
 def stack_experts(pws) -> PackedExperts:
@@ -1161,24 +1161,31 @@ def stack_experts(pws) -> PackedExperts:
                          torch.stack([p.meta for p in pws]), torch.stack([p.dense for p in pws]))
 
 
-def _check_experts(X, experts, groups, w_scales, x_scale, top, gathered):
-    """Shapes, types and devices of a grouped product's inputs."""
-    e0 = experts[0]
-    _check_x(X, SPENSE_FP8_E4M3FN, e0.K)
+def _check_expert_scale(s, w, dev):
+    if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (w.count, w.N) or not s.is_contiguous()
+                          or s.device != dev):
+        raise ValueError(f"w_scale must be a contiguous fp32 tensor of shape {(w.count, w.N)} on {dev}")
+
+
+def _check_experts(X, experts, w_scales, x_scale, count, dev):
+    """Types, shapes and devices of a grouped product's activations and weights."""
+    _check_x(X, SPENSE_FP8_E4M3FN, experts[0].K)
+    for w, s in zip(experts, w_scales):
+        if w.count != count:
+            raise ValueError(f"groups are over {count} experts, the weights over {w.count}")
+        if w.device != dev:
+            raise ValueError(f"the weights are on {w.device}, expected {dev}")
+        _check_expert_scale(s, w, dev)
+    _check_scale(x_scale, X.shape[0], dev, "x_scale")
+
+
+def _check_groups(X, groups, top, gathered, dev):
+    _on_gpu(dev)
+    _same_device(groups, dev)
     if top < 1:
         raise ValueError(f"top = {top}")
-    dev = X.device
-    _same_device(groups, dev)
     if X.shape[0] * (1 if gathered else top) != groups.n:
         raise ValueError(f"X has {X.shape[0]} rows, the groups {groups.n}")
-    for w, s in zip(experts, w_scales):
-        if groups.groups != w.count:
-            raise ValueError(f"groups are over {groups.groups} experts, the weights over {w.count}")
-        _on_gpu(dev, w.dense)
-        if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (w.count, w.N) or not s.is_contiguous()
-                              or s.device != dev):
-            raise ValueError(f"w_scale must be a contiguous fp32 tensor of shape {(w.count, w.N)} on {dev}")
-    _check_scale(x_scale, X.shape[0], dev, "x_scale")
 
 
 def gemm_experts(X: torch.Tensor, experts, groups: RowGroups, w_scales=None, x_scale=None, *, top: int = 1,
@@ -1196,8 +1203,9 @@ def gemm_experts(X: torch.Tensor, experts, groups: RowGroups, w_scales=None, x_s
         w_scales = [None] * k
     if len(w_scales) != k:
         raise ValueError("one w_scale per weight")
-    _check_experts(X, experts, groups, w_scales, x_scale, top, gathered)
     n, dev = groups.n, X.device
+    _check_groups(X, groups, top, gathered, dev)
+    _check_experts(X, experts, w_scales, x_scale, groups.groups, dev)
     if outs is None:
         outs = [None] * k
     if len(outs) != k:
@@ -1220,8 +1228,9 @@ def gemm_experts_glu_fp8(X: torch.Tensor, gate: PackedExperts, up: PackedExperts
     """The producer half of a GLU MLP of experts (spense_gemm_experts_glu_fp8): h = up * silu(gate) of every
     position, quantised per row.  Returns (codes uint8 n x N, scales fp32 n), the input of the experts'
     down projection (``gathered``); those of positions in no group are unspecified."""
-    _check_experts(X, [gate, up], groups, [gate_scale, up_scale], x_scale, top, gathered)
     n, N, dev = groups.n, gate.N, X.device
+    _check_groups(X, groups, top, gathered, dev)
+    _check_experts(X, (gate, up), (gate_scale, up_scale), x_scale, groups.groups, dev)
     q = torch.empty((n, N), dtype=torch.uint8, device=dev)
     scales = torch.empty(n, dtype=torch.float32, device=dev)
     ws = workspace or _CallScratch(dev)
@@ -1239,14 +1248,44 @@ def mlp_experts(X: torch.Tensor, x_scale: torch.Tensor, idx: torch.Tensor, weigh
                 out_f32: bool = False, workspace: Workspace | None = None) -> torch.Tensor:
     """A GLU MLP of experts (``mlp`` of each token's choices, summed): idx T x top int32 names each
     token's experts (outside [0, count): none), weights T x top fp32 what each counts.  The rows are
-    grouped by expert, gate and up computed for every position, H = up * silu(gate) quantised per row,
-    down computed and each token's rows summed in fp32.  X: T x K fp8 codes with x_scale."""
+    grouped by expert (group_rows), gate and up computed for every position with H = up * silu(gate)
+    quantised per row (gemm_experts_glu_fp8), down computed in fp32 (gemm_experts) and each token's rows
+    summed (combine_rows).  X: T x K fp8 codes with x_scale.  What lies between the steps is in one
+    scratch buffer, of this call or of ``workspace``."""
     if idx.dim() != 2 or idx.shape[0] != X.shape[0] or weights.shape != idx.shape:
         raise ValueError("idx and weights must be T x top")
-    top = idx.shape[1]
+    T, top = idx.shape
     if top < 1:
         raise ValueError("at least one expert per token")
-    groups = group_rows(idx.reshape(-1), gate.count)
-    Hq, sh = gemm_experts_glu_fp8(X, gate, up, groups, gate_scale, up_scale, x_scale, top=top, workspace=workspace)
-    D, = gemm_experts(Hq, [down], groups, [down_scale], sh, gathered=True, out_f32=True)
-    return combine_rows(D, groups, weights, top, out=out, out_f32=out_f32)
+    if idx.dtype != torch.int32 or not idx.is_contiguous():
+        raise ValueError("idx must be contiguous int32")
+    if weights.dtype != torch.float32 or not weights.is_contiguous():
+        raise ValueError("weights must be contiguous fp32")
+    dev, E, I, H, n = X.device, gate.count, gate.N, down.N, T * top
+    if down.count != E or down.K != I:
+        raise ValueError(f"down must be of {E} experts with K = {I}")
+    _on_gpu(dev, idx, weights, down.dense)
+    _check_experts(X, (gate, up), (gate_scale, up_scale), x_scale, E, dev)
+    _check_expert_scale(down_scale, down, dev)
+    out = _out(out, T, H, out_f32, dev)
+    sizes = (4 * (2 * n + E + 1), n * I, 4 * n, 4 * n * H, spense_gemm_experts_glu_fp8_workspace_size(n, E, I))
+    at, total = [], 0
+    for size in sizes:
+        at.append(total)
+        total += -(-size // 256) * 256
+    ws = workspace or _CallScratch(dev)
+    with _device(dev):
+        base, _ = ws.get(total)
+        groups, q, qs, d, glu = (base + o for o in at)
+        order, inverse, offsets = groups, groups + 4 * n, groups + 8 * n
+        st = _stream(dev)
+        _check(spense_group_rows(_ptr(idx), n, E, order, inverse, offsets, st))
+        _check(spense_gemm_experts_glu_fp8(_ptr(X), T, _ld16(X), _ptr(x_scale), order, top, offsets, n, E,
+                                           ctypes.byref(gate.desc), ctypes.byref(up.desc), _ptr(gate_scale),
+                                           _ptr(up_scale), q, I, qs, glu, sizes[4], st))
+        _check(spense_gemm_experts(q, n, I, qs, None, 1, offsets, n, E, 1, down.desc_array,
+                                   None if down_scale is None else (ctypes.c_void_p * 1)(_ptr(down_scale)),
+                                   (ctypes.c_void_p * 1)(d), (ctypes.c_int64 * 1)(H), SPENSE_OUT_F32, st))
+        _check(spense_combine_rows(d, SPENSE_F32, n, H, inverse, _ptr(weights), T, top, H, _ptr(out), _ld(out),
+                                   SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, st))
+    return out

@@ -193,7 +193,7 @@ int spense_group_rows(const int32_t* idx, int64_t n, int32_t groups, int32_t* or
     hipLaunchKernelGGL(spense::group_rows_kernel<256>, dim3(1), dim3(256), 0, stream, idx, n, groups, bits, order, inverse,
                        offsets);
   else
-    hipLaunchKernelGGL(spense::group_rows_kernel<1024>, dim3((unsigned)((n + 1023) / 1024)), dim3(1024), 0, stream, idx, n,
+    hipLaunchKernelGGL(spense::group_rows_kernel<1024>, dim3((unsigned)(n > 0 ? (n + 1023) / 1024 : 1)), dim3(1024), 0, stream, idx, n,
                        groups, bits, order, inverse, offsets);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return api_fail(SPENSE_ERR_HIP, "group rows launch failed: %s", hipGetErrorString(e));
