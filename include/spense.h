@@ -535,12 +535,14 @@ int spense_obs_prune_24(float* W, int64_t ldw, int64_t N, int64_t K, const float
  * row of K shared by all tokens.  post_weight, weight: K of w_type.  Types SPENSE_BF16 or
  * SPENSE_F32.  residual may be x itself and normed may be y itself (same pointer, leading
  * dimension and type); other overlaps of an output are not allowed.  A row of zeros gives
- * codes of zero with scale 1; NaN and infinities go where the formulas take them (NaN codes
- * are 0xff).
- * Any K and alignment of whole elements; 16-byte aligned rows (8 for q) with K % 8 == 0 take
- * the fast path.  One workgroup per row.  Asynchronous, allocates nothing.
+ * codes of zero with scale 1 (with eps = 0 it is NaN); NaN and infinities go where the formulas
+ * take them, a NaN code being 0xff, and stay in their rows.
+ * Any K and any alignment of whole elements; rows of 8 to 32768 are read once.  (M + 255) t
+ * below 2^32 with t = 16, 32, 64 for K in [8, 128], (128, 256], (256, 512] and 1024 for other K.
+ * Asynchronous, allocates nothing.
  * SPENSE_ERR_ARG for a NULL x, no output, q without scales, a gate or post_weight without y,
- * sizes below 0 or above 2^31-1, ld below K, unknown types, a negative or non-finite eps;
+ * M below 0 or too large, K below 1 or above 2^31-1, residual in the place of y or normed, normed in the
+ * place of x, ld below K, unknown types, a negative or non-finite eps;
  * SPENSE_ERR_ALIGN for an operand not aligned to its elements.
  */
 typedef struct spense_block_norm_t {
@@ -569,8 +571,9 @@ typedef struct spense_block_norm_t {
 
 int spense_block_norm(const spense_block_norm_t* args, hipStream_t stream);
 
-/* The most groups (experts, adapters) of one spense_group_rows call. */
+/* The most groups (experts, adapters) and rows of one spense_group_rows call. */
 #define SPENSE_MAX_GROUPS 1024
+#define SPENSE_MAX_GROUP_ROWS (1 << 20)
 
 /*
  * Group n rows by an index, as the expert and adapter calls below take them: a stable sort.
@@ -581,7 +584,7 @@ int spense_block_norm(const spense_block_norm_t* args, hipStream_t stream);
  *   inverse: n int32 or NULL; the position of each entry, -1 where its idx names no group.
  * idx: n int32 on the device, any values.  Outputs must not overlap idx or each other.  The
  * result depends on idx only.  One launch; asynchronous, allocates nothing.
- * SPENSE_ERR_ARG for NULL pointers, n below 0 or above 2^31-1, groups outside [1,
+ * SPENSE_ERR_ARG for NULL pointers, n outside [0, SPENSE_MAX_GROUP_ROWS], groups outside [1,
  * SPENSE_MAX_GROUPS].
  */
 int spense_group_rows(const int32_t* idx, int64_t n, int32_t groups, int32_t* order, int32_t* inverse, int32_t* offsets,
@@ -594,8 +597,8 @@ int spense_group_rows(const int32_t* idx, int64_t n, int32_t groups, int32_t* or
  * int32 (entries outside [0, n), e.g. -1, add nothing; a token without any gives zeros);
  * weights: T * top fp32 or NULL (ones).  Y: T x N, bf16 or fp32 (SPENSE_OUT_F32), leading
  * dimension ldy; it must not overlap D.  Asynchronous, allocates nothing.  SPENSE_ERR_ARG for
- * NULL pointers, bad sizes, types or flags, ld below N; SPENSE_ERR_ALIGN for a D or Y not
- * aligned to its elements.
+ * NULL pointers, bad sizes (n or T * top above SPENSE_MAX_GROUP_ROWS, T x N too large for a launch),
+ * types or flags, Y = D, ld below N; SPENSE_ERR_ALIGN for a D or Y not aligned to its elements.
  */
 int spense_combine_rows(const void* D, int32_t d_type, int64_t n, int64_t ldd, const int32_t* inverse,
                         const float* weights, int64_t T, int32_t top, int64_t N, void* Y, int64_t ldy, uint32_t out_flags,
@@ -635,7 +638,8 @@ size_t spense_adapters_workspace_size(int64_t M, const spense_adapters_t* pool);
  * rounded once.  The order of the sums depends on the sizes only.  Two launches, asynchronous;
  * ws is scratch between them, caller-owned; calls that overlap on one workspace race.
  * order entries outside [0, M) are skipped, offsets are clamped to [0, M].
- * SPENSE_ERR_ARG for NULL pointers, bad sizes or types, an R or count outside the limits above,
+ * SPENSE_ERR_ARG for NULL pointers, bad sizes (M above SPENSE_MAX_GROUP_ROWS, M x N too large for a
+ * launch) or types, an R or count outside the limits above,
  * ld below the row length, a Y = base of another type or pitch, X or one adapter of 2 GiB or
  * more; SPENSE_ERR_ALIGN for X, A, B or ws not 16-byte aligned (ldx a multiple of 16 bytes),
  * K % 32, base or Y not aligned to its elements; SPENSE_ERR_WS for a missing or small workspace.
@@ -662,8 +666,8 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
  * dimension ldy[i].  fp32 sums whose order depends on the sizes only, rounded once.
  * order entries whose row is outside [0, rows_x) give zeros, offsets are clamped to [0, n].
  * Asynchronous, allocates nothing.  SPENSE_ERR_ARG for NULL pointers, weights outside [1, 2],
- * count outside [1, SPENSE_MAX_GROUPS], top below 1, bad sizes or flags, mixed or unsupported
- * weights, K = 0, ld below the row length, an X or one expert's buffer of 2 GiB or more;
+ * count outside [1, SPENSE_MAX_GROUPS], top below 1, bad sizes (n above SPENSE_MAX_GROUP_ROWS, n x N
+ * too large for a launch) or flags, Y[1] = Y[0], mixed or unsupported weights, K = 0, ld below the row length, an X or one expert's buffer of 2 GiB or more;
  * SPENSE_ERR_ALIGN for a misaligned X, Y or weight.
  */
 int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order, int32_t top,

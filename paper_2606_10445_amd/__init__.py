@@ -41,6 +41,7 @@ SPENSE_LAYOUT_ROWMAJOR = 0
 SPENSE_LAYOUT_TILED = 1
 SPENSE_NOALLOC_SCRATCH_BYTES = 16 << 20
 SPENSE_MAX_GROUPS = 1024
+SPENSE_MAX_GROUP_ROWS = 1 << 20
 
 EXPORTS = ["spense_abi_version", "spense_set_log", "spense_last_error", "spense_layout", "spense_tiled_layout",
            "spense_compress_workspace_size", "spense_compress", "spense_decompress", "spense_tile",
@@ -936,8 +937,10 @@ def block_norm(x: torch.Tensor, y: torch.Tensor | None = None, *, post_weight=No
     ``normed``; codes uint8 M x K and scales fp32 M of n where ``quantize``).  gate: K entries shared by
     all tokens, or M x K, of y's type; post_weight, weight: K entries of one type, bf16 or fp32.
     residual_out may be x and normed_out may be y."""
-    _row_major(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be a 2-D row-major tensor")
     M, K = x.shape
+    _rows_of(x, "x", (M, K))
     dev = x.device
     xt = _act_type(x)
     if y is None:
@@ -1046,8 +1049,10 @@ def combine_rows(D: torch.Tensor, groups: RowGroups, weights: torch.Tensor | Non
     """Y[t] = sum_j weights[t, j] * D[position of row t * top + j], fp32 sums in order of j
     (spense_combine_rows).  D: n x N in the positions of ``groups`` (bf16 or fp32); weights: T x top
     fp32 with T = n / top.  Rows in no group add nothing."""
-    _row_major(D, "D")
+    if D.dim() != 2:
+        raise ValueError("D must be a 2-D row-major tensor")
     n, N = D.shape
+    _rows_of(D, "D", (n, N))
     if top < 1 or groups.n != n or n % top:
         raise ValueError(f"D has {n} rows, the groups {groups.n}; both must be T * top with top = {top}")
     T = n // top
@@ -1091,14 +1096,12 @@ def add_adapters(base: torch.Tensor, X: torch.Tensor, pool: AdapterPool, groups:
     base: M x N, bf16 or fp32, the projection's output; X: M x K, bf16 or fp8 codes with x_scale;
     groups: group_rows of the tokens' adapter indices over pool.count groups (tokens of no group get
     base).  out may be base."""
-    _row_major(X, "X")
     M = X.shape[0]
+    _rows_of(X, "X", (M, pool.K))
     dev = X.device
     xt = SPENSE_BF16 if X.dtype == torch.bfloat16 else _act_code(X)
     if xt is None or X.dtype in (torch.int16, torch.uint16):
         raise ValueError(f"X is {X.dtype}; adapters take fp8 codes (uint8) or bfloat16")
-    if X.shape[1] != pool.K:
-        raise ValueError(f"X.shape[1] = {X.shape[1]} != K = {pool.K}")
     _rows_of(base, "base", (M, pool.N))
     bt = _act_type(base)
     if groups.n != M or groups.groups != pool.count:

@@ -62,10 +62,10 @@ __device__ __forceinline__ v4f mma_bf16(v4i a, v4i b, v4f c) {
 }
 
 // V partials of one tile (16 CT tokens), RT * 16 ranks from 16 RT * blockIdx.z and one K
-// slice (1, 2, 4 or 8 of them; workgroups of XCD x = blockIdx.x % 8 all take slice x % slices, so that
-// an XCD reads that part of the adapters and activations only).  A step is 64 columns: lane group q takes columns [16 q, 16 q + 16) of both operands
-// (a permutation of K inside the step, the same on both sides), which makes a row's step one
-// 128-byte line of A.
+// slice (1, 2, 4 or 8 of them; workgroups of XCD x = blockIdx.x % 8 all take slice x % slices, so
+// that an XCD reads that part of the adapters and activations only).  A step is 64 columns: lane group q
+// takes columns [16 q, 16 q + 16) of both operands (a permutation of K inside the step, the same on
+// both sides), which makes a row's step one 128-byte line of A.
 template <bool FP8, int RT, int CT, int NW>
 __global__ __launch_bounds__(64 * NW) void adapter_shrink_kernel(AdapterArgs a) {
   RowTile t;
@@ -418,7 +418,7 @@ using spense::api_fail;
 extern "C" {
 
 size_t spense_adapters_workspace_size(int64_t M, const spense_adapters_t* pool) {
-  if (!pool || M < 1 || M > INT32_MAX || spense::bad_pool(*pool)) return 0;
+  if (!pool || M < 1 || M > SPENSE_MAX_GROUP_ROWS || spense::bad_pool(*pool)) return 0;
   return (size_t)spense::k_slices(M, pool->count, pool->K, pool->R) * (size_t)M * (size_t)pool->R * 4;
 }
 
@@ -438,7 +438,8 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   if (base_type != SPENSE_BF16 && base_type != SPENSE_F32)
     return api_fail(SPENSE_ERR_ARG, "base_type %d is not bf16 or f32", base_type);
   if (out_flags & ~1u) return api_fail(SPENSE_ERR_ARG, "unknown out_flags 0x%x", out_flags);
-  if (M < 0 || M > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "bad M");
+  if (M < 0 || M > SPENSE_MAX_GROUP_ROWS)
+    return api_fail(SPENSE_ERR_ARG, "M=%lld outside [0, %d]", (long long)M, SPENSE_MAX_GROUP_ROWS);
   if (M == 0) return spense::api_ok();
   if (!X || !order || !offsets || !P.A || !P.B || !base || !Y) return api_fail(SPENSE_ERR_ARG, "NULL pointer");
   if (ldx < P.K || ldb < P.N || ldy < P.N) return api_fail(SPENSE_ERR_ARG, "leading dimension below the row length");
@@ -464,7 +465,7 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   int steps = T == 64 ? 4 : 8;
   while (steps > 2 && tiles_used * ((P.N + 128 * steps - 1) / (128 * steps)) < 512) steps /= 2;
   const int64_t nblocks = (P.N + 128 * steps - 1) / (128 * steps);
-  if (all_tiles * nblocks > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "M x N too large for the grid");
+  if (!spense::grid_fits(all_tiles * nblocks, 256)) return api_fail(SPENSE_ERR_ARG, "M x N too large for the grid");
   const size_t need = spense_adapters_workspace_size(M, pool);
   if (!ws || ws_bytes < need) return api_fail(SPENSE_ERR_WS, "workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
   if (at(ws) % 16) return api_fail(SPENSE_ERR_ALIGN, "workspace must be 16-byte aligned");

@@ -293,8 +293,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Kernels of the grouped products.
 enum Kernel { kRows16, kRows32, kRows64, kMid, kBig };
 
-// Chunks of 512 columns that experts_stream_kernel takes: up to K = 3072, beyond which waiting for
-// all activations costs more than the pipeline's drains (2048 x 4096, 8 rows an expert: 15.1 us
+// Chunks of 512 columns that experts_stream_kernel takes, beyond which waiting for all activations
+// costs more than the pipeline's drains (2048 x 4096, 8 rows an expert: 15.1 us
 // against 10.5; 4096 x 2560 22.3 against 23.9; 5120 x 1536 39 against 48).
 constexpr int64_t kStreamChunks = 6;
 
@@ -355,7 +355,7 @@ int check_call(Call& c, const void* X, int64_t rows_x, int64_t ldx, const float*
   if (count < 1 || count > SPENSE_MAX_GROUPS)
     return api_fail(SPENSE_ERR_ARG, "count=%d outside [1, %d]", count, SPENSE_MAX_GROUPS);
   if (!packed) return api_fail(SPENSE_ERR_ARG, "NULL array");
-  if (n < 0 || n > INT32_MAX || rows_x < 0 || rows_x > INT32_MAX)
+  if (n < 0 || n > SPENSE_MAX_GROUP_ROWS || rows_x < 0 || rows_x > INT32_MAX)
     return api_fail(SPENSE_ERR_ARG, "bad n=%lld rows_x=%lld", (long long)n, (long long)rows_x);
   if (top < 1) return api_fail(SPENSE_ERR_ARG, "top=%d", top);
   for (int i = 0; i < weights; ++i) {
@@ -433,7 +433,7 @@ int launch_tiles(Call& c, bool big, float* pmax, int64_t pmax_ld, hipStream_t st
     blocks += R.nrb;
   }
   g.groups = (int32_t)blocks, g.hg0 = g.groups;
-  if (spense::most_tiles(c.er.n, c.er.count, false, big ? 256 : 128) * blocks > INT32_MAX - 8)
+  if (!spense::grid_fits(spense::most_tiles(c.er.n, c.er.count, false, big ? 256 : 128) * blocks + 8, big ? 512 : 768))
     return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
   int rc = spense::api_check_device();
   if (rc) return rc;
@@ -470,7 +470,8 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
     // row tiles of a wave: rounds of the workgroups that run at once (three of four waves or one of eight a
     // CU) times a workgroup's time, its start as long as 90 KB of a CU's weights; tiles as even groups give
     const int64_t used = c.er.count < c.er.n ? c.er.count : c.er.n, tiles_even = used * ceil_div(c.er.n / used, 16 * ct);
-    const int64_t at_once = 256 * (ct == 1 ? 3 : 1), step = (ct == 1 ? 192 : 128) * c.K * 23 / 32;  // a CU's bytes for one row tile a wave, a quarter of them dense
+    const int64_t at_once = 256 * (ct == 1 ? 3 : 1);
+    const int64_t step = (ct == 1 ? 192 : 128) * c.K * 23 / 32;  // a CU's bytes for one row tile a wave, a quarter dense
     int64_t best = 0;
     for (int64_t per = 1; per <= spense::kStreamTiles; ++per) {
       const int64_t cost = ceil_div(tiles_even * wgs(per), at_once) * (90000 + per * step);
@@ -481,7 +482,7 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
     a.wgs = (int32_t)ceil_div(tiles, wv);
   }
   const int64_t grid = most * a.wgs;
-  if (grid > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
+  if (!spense::grid_fits(grid, 64 * wv)) return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
   int rc = spense::api_check_device();
   if (rc) return rc;
   const hipError_t e = stream_kernel ? (ct == 1   ? spense::launch_stream<1, 4>(a, c.er, grid, (int)lds, stream)
@@ -521,7 +522,7 @@ int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float*
   if (c.er.n == 0) return spense::api_ok();
   const bool f32 = (out_flags & SPENSE_OUT_F32) != 0;
   for (int i = 0; i < weights; ++i) {
-    if (!Y[i]) return api_fail(SPENSE_ERR_ARG, "Y[%d] is NULL", i);
+    if (!Y[i] || (i && Y[i] == Y[0])) return api_fail(SPENSE_ERR_ARG, "Y[%d] is NULL or Y[0]", i);
     if (ldy[i] < c.N) return api_fail(SPENSE_ERR_ARG, "ldy[%d] < N", i);
     if (reinterpret_cast<uintptr_t>(Y[i]) % (f32 ? 4 : 2)) return api_fail(SPENSE_ERR_ALIGN, "Y[%d] misaligned", i);
     if (n * ldy[i] > (int64_t)1 << 40) return api_fail(SPENSE_ERR_ARG, "Y[%d] too large", i);
@@ -532,7 +533,7 @@ int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float*
 }
 
 size_t spense_gemm_experts_glu_fp8_workspace_size(int64_t n, int32_t count, int64_t N) {
-  if (n < 1 || n > INT32_MAX || N < 1 || N > INT32_MAX || count < 1 || count > SPENSE_MAX_GROUPS) return 0;
+  if (n < 1 || n > SPENSE_MAX_GROUP_ROWS || N < 1 || N > INT32_MAX || count < 1 || count > SPENSE_MAX_GROUPS) return 0;
   if (big_tiles(n, count, N, 2)) return (size_t)(glu_rows_bytes(n, N) + n * glu_maxima(N) * 4);
   return (size_t)(2 * glu_rows_bytes(n, N));
 }
@@ -554,7 +555,7 @@ int spense_gemm_experts_glu_fp8(const void* X, int64_t rows_x, int64_t ldx, cons
   if (!ws || ws_bytes < need)
     return api_fail(SPENSE_ERR_WS, "workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
   if (reinterpret_cast<uintptr_t>(ws) % 256) return api_fail(SPENSE_ERR_ALIGN, "workspace must be 256-byte aligned");
-  if (n * ceil_div(c.N, 2048) > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "n x N too large for the quantisation grid");
+  if (!spense::grid_fits(n * ceil_div(c.N, 2048), 256)) return api_fail(SPENSE_ERR_ARG, "n x N too large for the quantisation grid");
   const int64_t ld = glu_ld(c.N), half = glu_rows_bytes(n, c.N);
   float* const H = static_cast<float*>(ws);
   float* const second = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + half);

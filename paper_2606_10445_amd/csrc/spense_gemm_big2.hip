@@ -51,6 +51,13 @@ constexpr int kB2SWgt = kB2RowTiles * 1024 + kB2RowTiles * 256;      // 2:4 valu
 constexpr int kB2DWgt = kB2RowTiles * 2048;                          // both dense halves of one step
 constexpr int kB2Lds = 2 * kB2XSlot + (4 * kB2SWgt > 3 * kB2DWgt ? 4 * kB2SWgt : 3 * kB2DWgt);
 
+// Keeps a kernel argument in its scalar registers: the compiler else loads it again where it is
+// used, in the prologue's and the epilogue's branches one memory round trip after the other.
+template <typename T>
+__device__ __forceinline__ void keep_scalar(T& v) {
+  asm volatile("" : "+s"(v));
+}
+
 // MODE 1: a grouped launch (several weights sharing X and K): up to kMaxRegions regions, each
 // reading its weight's buffers, output and scales from a.mat[R.mat].
 // MODE 2: the gate / up pair (a.mat[0], a.mat[1], one geometry): a workgroup takes the same 128
@@ -59,13 +66,6 @@ constexpr int kB2Lds = 2 * kB2XSlot + (4 * kB2SWgt > 3 * kB2DWgt ? 4 * kB2SWgt :
 // maxima.  G and U written in fp32 and read again cost a 25600 x 5120 pair 420 MB more per
 // 2048 tokens than H does: GEMM and GLU quantisation 450 + 124 us, now 366 + 46 (the
 // quantisation reads and writes 5.7 TB/s); the whole MLP at M = 256 142 -> 126 us.
-// Keeps a kernel argument in its scalar registers: the compiler else loads it again where it is
-// used, in the prologue's and the epilogue's branches one memory round trip after the other.
-template <typename T>
-__device__ __forceinline__ void keep_scalar(T& v) {
-  asm volatile("" : "+s"(v));
-}
-
 enum { kB2Plain = 0, kB2Grouped = 1, kB2Glu = 2 };
 
 // RG: rows grouped by expert, as in mid_body, tiles of up to 256 positions.

@@ -6,8 +6,9 @@
 // order).  Inside a wave a lane finds the lanes with its key by ballots over the key's bits; its
 // rank is the number of lower ones.  The order is the index order, whatever the timing.
 //
-// Latency-bound at decode sizes (n = 64: 3.9 us).  One workgroup walking all entries with ballots
-// took 22 us for n = 16384, its one CU's vector instructions the bound.
+// Latency-bound at decode sizes (n = 64: 3.7 us); n = 16384 takes 8 us (one workgroup walking all
+// entries with ballots 22, its CU's vector instructions the bound), 65536 18, 2^20 0.65 ms: the
+// counting grows with n^2 / 1024, so that is the most a call takes.
 #include <hip/hip_runtime.h>
 
 #include "spense.h"
@@ -181,7 +182,8 @@ extern "C" {
 
 int spense_group_rows(const int32_t* idx, int64_t n, int32_t groups, int32_t* order, int32_t* inverse, int32_t* offsets,
                       hipStream_t stream) {
-  if (n < 0 || n > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "bad n=%lld", (long long)n);
+  if (n < 0 || n > SPENSE_MAX_GROUP_ROWS)
+    return api_fail(SPENSE_ERR_ARG, "n=%lld outside [0, %d]", (long long)n, SPENSE_MAX_GROUP_ROWS);
   if (groups < 1 || groups > SPENSE_MAX_GROUPS)
     return api_fail(SPENSE_ERR_ARG, "groups=%d outside [1, %d]", groups, SPENSE_MAX_GROUPS);
   if (!offsets || (n > 0 && (!idx || !order))) return api_fail(SPENSE_ERR_ARG, "NULL pointer");
@@ -204,7 +206,8 @@ int spense_combine_rows(const void* D, int32_t d_type, int64_t n, int64_t ldd, c
                         const float* weights, int64_t T, int32_t top, int64_t N, void* Y, int64_t ldy, uint32_t out_flags,
                         hipStream_t stream) {
   if (d_type != SPENSE_BF16 && d_type != SPENSE_F32) return api_fail(SPENSE_ERR_ARG, "d_type %d is not bf16 or f32", d_type);
-  if (n < 0 || T < 0 || N < 0 || top < 1 || n > INT32_MAX || T > INT32_MAX || N > INT32_MAX || T * top > INT32_MAX)
+  if (n < 0 || T < 0 || N < 0 || top < 1 || n > SPENSE_MAX_GROUP_ROWS || T > SPENSE_MAX_GROUP_ROWS || N > INT32_MAX ||
+      T * top > SPENSE_MAX_GROUP_ROWS)
     return api_fail(SPENSE_ERR_ARG, "bad n=%lld T=%lld top=%d N=%lld", (long long)n, (long long)T, top, (long long)N);
   if (out_flags & ~1u) return api_fail(SPENSE_ERR_ARG, "unknown out_flags 0x%x", out_flags);
   if (T == 0 || N == 0) return spense::api_ok();
@@ -213,7 +216,8 @@ int spense_combine_rows(const void* D, int32_t d_type, int64_t n, int64_t ldd, c
   const int64_t ds = d_type == SPENSE_BF16 ? 2 : 4, ys = (out_flags & SPENSE_OUT_F32) ? 4 : 2;
   const uintptr_t dp = reinterpret_cast<uintptr_t>(D), yp = reinterpret_cast<uintptr_t>(Y);
   if (dp % ds || yp % ys) return api_fail(SPENSE_ERR_ALIGN, "D or Y misaligned");
-  if (T * ((N + 255) / 256) > INT32_MAX) return api_fail(SPENSE_ERR_ARG, "T x N too large for the grid");
+  if (D == Y) return api_fail(SPENSE_ERR_ARG, "Y in the place of D");
+  if (!spense::grid_fits(T * ((N + 255) / 256), 256)) return api_fail(SPENSE_ERR_ARG, "T x N too large for the grid");
   int rc = spense::api_check_device();
   if (rc) return rc;
   // four columns a thread where D's and Y's quads are aligned

@@ -144,6 +144,9 @@ int api_ok();
 int api_check_device();
 int api_check_packed(const spense_packed_t* P);
 
+// Whether a launch of this many workgroups fits the runtime's 32-bit count of work items.
+inline bool grid_fits(int64_t workgroups, int64_t threads) { return workgroups <= UINT32_MAX / threads; }
+
 // Y for the rows of K-sliced regions: the sum of their fp32 partials in slice order, then
 // the epilogue (after launch_gemm, on the same stream).
 hipError_t launch_splitk_reduce(const GemmArgs& a, hipStream_t s);

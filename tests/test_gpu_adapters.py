@@ -141,6 +141,22 @@ def test_in_place_and_strides(S, N, dt):
     assert torch.equal(y[1].cpu().contiguous().view(bits), t[5][1].view(bits))
 
 
+@pytest.mark.parametrize("M,N", [(6, 130), (200, 520)])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_rows_far_apart(S, M, N, dt):
+    """Offsets past 32 bits in base and out."""
+    K, R, count = 64, 16, 2
+    t = inputs(13, M, K, N, R, count, "bf16", dt)
+    f32 = dt == "f32"
+    ref = call(S, t, count, out_f32=f32)
+    pool = S.AdapterPool(*(v.cuda() for v in t[2:5]))
+    pitch = -(-(9 << 29) // M) + 3
+    far = torch.empty((M - 1) * pitch + N, dtype=t[5].dtype, device="cuda").as_strided((M, N), (pitch, 1))
+    far.copy_(t[5])
+    S.add_adapters(far, t[0].cuda(), pool, S.group_rows(t[6].cuda(), count), out=far, out_f32=f32)
+    assert torch.equal(far.contiguous(), ref)
+
+
 def test_non_finite_tokens_stay_alone(S):
     M, K, N, R = 20, 256, 64, 16
     t = inputs(3, M, K, N, R, 1, "bf16", "f32", idx=torch.zeros(M))
@@ -230,7 +246,8 @@ def test_binding_refuses(S):
     for bad in ((A.float(), B), (A, B[:, :, :4]), (A[:1], B), (A.transpose(1, 2), B), (A, B, sc[:1]), (A, B.cpu())):
         with pytest.raises((ValueError, TypeError)):
             S.AdapterPool(*bad)
-    for kw in (dict(X=X[:4]), dict(X=X.float()), dict(X=X[:, :32]), dict(base=bd[:, :8]), dict(base=bd.half()),
+    for kw in (dict(X=X[:4]), dict(X=X.float()), dict(X=X[:, :32]), dict(X=X[0].expand(8, 64)),
+               dict(base=bd[0].expand(8, 32)), dict(base=bd[:, :8]), dict(base=bd.half()),
                dict(groups=S.group_rows(idx, 3)), dict(groups=S.group_rows(idx[:4], 2)), dict(x_scale=sc),
                dict(out=torch.zeros(8, 31, dtype=torch.bfloat16, device="cuda")), dict(X=X.view(torch.int16))):
         with pytest.raises((ValueError, TypeError)):

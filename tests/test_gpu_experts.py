@@ -218,6 +218,38 @@ def test_non_finite_rows_stay_alone(S):
         assert torch.equal(y[keep], clean[keep]) and torch.any(torch.isnan(y[at]))
 
 
+@pytest.mark.parametrize("T,E,N,K", [(5, 2, 40, 128), (5, 2, 40, 3584), (40, 2, 70, 3584), (300, 2, 130, 128), (700, 1, 5602, 128)])
+@pytest.mark.parametrize("f32", [False, True])
+def test_outputs_far_apart(S, T, E, N, K, f32):
+    """Offsets of the output past 32 bits, in every kernel."""
+    g = torch.Generator().manual_seed(T + N)
+    pe, W, sc = weights(S, g, E, N, K, 0, 32, True)
+    x, xs = tokens(g, T, K, True)
+    groups = S.group_rows(choices(g, "even", T, 1, E).reshape(-1).cuda(), E)
+    pitch = -(-(9 << 29) // T) + 3
+    dt = torch.float32 if f32 else torch.bfloat16
+    y = torch.empty((T - 1) * pitch + N, dtype=dt, device="cuda").as_strided((T, N), (pitch, 1))
+    S.gemm_experts(x.view(torch.uint8).cuda(), [pe], groups, [sc.cuda()], xs.cuda(), outs=[y], out_f32=f32)
+    check(y.cpu(), groups.order.cpu(), groups.offsets.cpu(), x, xs, W, sc, 1, True, f32)
+
+
+@pytest.mark.parametrize("T,top,E,H,I", [(6, 2, 3, 256, 96), (300, 2, 4, 256, 96), (1300, 2, 2, 256, 1408)])
+def test_mlp_of_a_non_finite_token(S, T, top, E, H, I):
+    """A token whose scale is NaN and one with an infinite weight leave the others as they are."""
+    g = torch.Generator().manual_seed(T)
+    gate, up, down = weights(S, g, E, I, H, 0, 64, False), weights(S, g, E, I, H, 0, 64, False), weights(S, g, E, H, I, 1, 64, False)
+    x, xs = tokens(g, T, H, False)
+    idx, w = torch.randint(0, E, (T, top), generator=g, dtype=torch.int32), torch.rand(T, top, generator=g)
+    run = lambda xs, w: S.mlp_experts(x.view(torch.uint8).cuda(), xs.cuda(), idx.cuda(), w.cuda(), gate[0], up[0], down[0],  # noqa: E731
+                                      *(v[2].cuda() / 64 for v in (gate, up, down))).cpu()
+    clean = run(xs, w)
+    assert torch.all(torch.isfinite(clean))
+    xs[2], w[4, 1] = float("nan"), float("inf")
+    y = run(xs, w)
+    keep = [t for t in range(T) if t not in (2, 4)]
+    assert torch.equal(y[keep], clean[keep]) and torch.all(torch.isnan(y[2])) and not torch.any(torch.isfinite(y[4]))
+
+
 def decoded_glu(S, G, U):
     q, s = S.glu_quantize_fp8(G, U)
     return q.cpu().view(torch.float8_e4m3fn), s.cpu()

@@ -87,6 +87,19 @@ def test_combine_rows(S, T, top, N, dt, out_f32):
     assert torch.all((plain.cpu().double() - terms.sum(1)).abs() <= (top + 1) * U * terms.abs().sum(1))
 
 
+def test_combine_rows_far_apart(S):
+    """Offsets past 32 bits: rows of D and Y 2^30 elements apart."""
+    T, top, N, pitch = 3, 2, 260, 1 << 30
+    idx = torch.tensor([2, 0, 1, 1, 3, 0], dtype=torch.int32).cuda()
+    g = S.group_rows(idx, 3)
+    D = torch.empty(5 * pitch + N, device="cuda").as_strided((6, N), (pitch, 1))
+    D.copy_(torch.randn(6, N, generator=torch.Generator().manual_seed(3)))
+    w = torch.rand(T, top, generator=torch.Generator().manual_seed(4)).cuda()
+    out = torch.empty(2 * pitch + N, device="cuda").as_strided((T, N), (pitch, 1))
+    S.combine_rows(D, g, w, top=top, out=out, out_f32=True)
+    assert torch.equal(out, S.combine_rows(D.contiguous(), g, w, top=top, out_f32=True))
+
+
 def test_combine_rows_strided(S):
     T, top, N = 9, 2, 100
     gen = torch.Generator().manual_seed(5)
@@ -109,6 +122,7 @@ def test_binding_refuses(S):
     g = S.group_rows(idx, 4)
     D = torch.zeros(8, 16, device="cuda")
     for kw in (dict(D=D[:7]), dict(top=3), dict(top=0), dict(weights=torch.zeros(4, device="cuda")),
-               dict(weights=torch.zeros(8, device="cuda").half()), dict(out=torch.zeros(3, 16, device="cuda"))):
+               dict(weights=torch.zeros(8, device="cuda").half()), dict(D=D[0].expand(8, 16)),
+               dict(out=torch.zeros(3, 16, device="cuda"))):
         with pytest.raises(ValueError):
             S.combine_rows(**{"D": D, "groups": g, "top": 2, **kw})

@@ -139,6 +139,49 @@ def test_strides_and_in_place(S, K, pitch):
     assert torch.equal(xw[:, K:], x0[:, K:]) and torch.equal(yw[:, K:], y0[:, K:]) and torch.all(qw[:, K:] == 7)
 
 
+@pytest.mark.parametrize("K", [40, 1000, 1003, 4096, 8192, 8200])
+@pytest.mark.parametrize("wscale", [1.0, 1e-25, 1e22])
+def test_many_rows_codes(S, K, wscale):
+    """Codes of many rows are those that quantize_fp8 gives for the fp32 norm: ties, signed zeros, small
+    values and scales far from 1 among them."""
+    M = 600
+    x = rand(51, M, K) * torch.exp(rand(52, M, K) * 3)  # many values far below the row's largest
+    x[3, :7], x[4, 5] = -0.0, float("nan")
+    x[7] = torch.round(x[7].clamp(-8, 8))
+    w = (rand(53, K).abs() + 0.5) * wscale
+    o = S.block_norm(x.cuda(), weight=w.cuda(), normed=True)
+    q, s = S.quantize_fp8(o.normed)
+    assert torch.equal(q, o.codes) and torch.equal(s, o.scales)
+
+
+def test_many_rows_in_place(S):
+    """r over x and n over y with ragged last pieces and two pieces a thread."""
+    M, K = 700, 2051
+    x, y, w = rand(61, M, K).cuda(), rand(62, M, K).cuda(), (1 + rand(63, K, scale=0.1)).cuda()
+    ref = S.block_norm(x, y, post_weight=w, weight=w, normed=True)
+    o = S.block_norm(x, y, post_weight=w, weight=w, residual_out=x, normed_out=y)
+    assert o.residual.data_ptr() == x.data_ptr() and all(torch.equal(a, b) for a, b in zip(o, ref))
+
+
+@pytest.mark.parametrize("K", [300, 2056])
+def test_rows_far_apart(S, K):
+    """Offsets past 32 bits: rows 3 x 2^29 elements apart in every operand."""
+    M, pitch = 4, 3 << 29
+    x, y, g = rand(71, M, K), rand(72, M, K, dtype=torch.bfloat16), rand(73, M, K, dtype=torch.bfloat16)
+
+    def far(t):
+        v = torch.empty((M - 1) * pitch + K, dtype=t.dtype, device="cuda").as_strided((M, K), (pitch, 1))
+        v.copy_(t)
+        return v
+
+    ref = S.block_norm(x.cuda(), y.cuda(), gate=g.cuda(), normed=True)
+    q = torch.empty((M - 1) * pitch + K, dtype=torch.uint8, device="cuda").as_strided((M, K), (pitch, 1))
+    fx, fy = far(x), far(y)
+    o = S.block_norm(fx, fy, gate=far(g), residual_out=fx, normed_out=fy, codes_out=q)
+    for a, b in zip(o, ref):
+        assert torch.equal(a, b)
+
+
 def test_rows_do_not_touch_each_other(S):
     """A zero row, an infinity and a NaN stay in their rows."""
     M, K = 6, 512
@@ -182,9 +225,11 @@ def test_binding_refuses(S):
                dict(y=y, codes_out=torch.zeros(4, 16, dtype=torch.uint8, device="cuda"))):
         with pytest.raises((ValueError, TypeError)):
             S.block_norm(x, **kw)
-    with pytest.raises(ValueError):
-        S.block_norm(x.cpu())
-    with pytest.raises(S.SpenseError):
-        S.block_norm(x, eps=-1.0)
+    for bad in (x.cpu(), x[0].expand(4, 32), x.t(), x[0]):
+        with pytest.raises(ValueError):
+            S.block_norm(bad)
+    for kw in (dict(eps=-1.0), dict(y=y, residual_out=y.clone(), normed_out=x), dict(y=y, residual_out=y)):
+        with pytest.raises((S.SpenseError, ValueError)):
+            S.block_norm(x, **kw)
     empty = S.block_norm(torch.zeros(0, 32, device="cuda"), normed=True)
     assert empty.normed.shape == (0, 32) and empty.codes.shape == (0, 32)

@@ -13,7 +13,7 @@ def S():
 
 def norm_args(S, **kw):
     a = dict(M=4, K=64, x=A, ldx=64, x_type=2, y_type=2, y=A, ldy=64, gate=A, ldg=0, post_weight=A, weight=A, w_type=3,
-             residual_scale=1.0, eps=1e-6, residual=A, ldr=64, normed=A, ldn=64, q=A, ldq=64, scales=A)
+             residual_scale=1.0, eps=1e-6, residual=2 * A, ldr=64, normed=3 * A, ldn=64, q=A, ldq=64, scales=A)
     a.update(kw)
     return S.spense_block_norm_t(**a)
 
@@ -25,6 +25,8 @@ def norm_args(S, **kw):
     (dict(scales=None), -1), (dict(residual=None, normed=None, q=None, scales=None), -1), (dict(ldx=63), -1),
     (dict(ldy=1), -1), (dict(ldg=8), -1), (dict(ldr=0), -1), (dict(ldn=63), -1), (dict(ldq=63), -1),
     (dict(x=A + 1), -2), (dict(y=A + 1), -2), (dict(weight=A + 2), -2), (dict(normed=A + 1), -2), (dict(scales=A + 2), -2),
+    (dict(y=2 * A), -1), (dict(normed=2 * A), -1), (dict(x=3 * A), -1), (dict(M=1 << 28), -1),
+    (dict(M=1 << 22, K=520, ldx=520, ldy=520, ldr=520, ldn=520, ldq=520), -1), (dict(M=1 << 22, K=4), -1),
 ])
 def test_block_norm_refuses(S, kw, code):
     assert S.spense_block_norm(norm_args(S, **kw), None) == code
@@ -33,23 +35,23 @@ def test_block_norm_refuses(S, kw, code):
 
 def test_block_norm_of_nothing(S):
     assert S._lib.spense_block_norm(None, None) == -1
+    assert S.spense_block_norm(norm_args(S, K=0), None) == -1
     assert S.spense_block_norm(norm_args(S, M=0, x=None), None) == 0
-    assert S.spense_block_norm(norm_args(S, K=0, x=None), None) == 0
     assert S.spense_last_error() == ""
 
 
-@pytest.mark.parametrize("args", [(A, -1, 4, A, A, A), (A, 1 << 31, 4, A, A, A), (A, 8, 0, A, A, A), (A, 8, 1025, A, A, A),
-                                  (None, 8, 4, A, A, A), (A, 8, 4, None, A, A), (A, 8, 4, A, A, None)])
+@pytest.mark.parametrize("args", [(A, -1, 4, A, A, A), (A, (1 << 20) + 1, 4, A, A, A), (A, 8, 0, A, A, A),
+                                  (A, 8, 1025, A, A, A), (None, 8, 4, A, A, A), (A, 8, 4, None, A, A), (A, 8, 4, A, A, None)])
 def test_group_rows_refuses(S, args):
     assert S.spense_group_rows(*args, None) == -1
 
 
 def test_combine_rows_refuses(S):
-    good = dict(D=A, d_type=2, n=8, ldd=16, inverse=A, weights=A, T=4, top=2, N=16, Y=A, ldy=16, out_flags=0, stream=None)
+    good = dict(D=A, d_type=2, n=8, ldd=16, inverse=A, weights=A, T=4, top=2, N=16, Y=2 * A, ldy=16, out_flags=0, stream=None)
     for kw, code in ((dict(D=None), -1), (dict(inverse=None), -1), (dict(Y=None), -1), (dict(d_type=1), -1),
                      (dict(n=-1), -1), (dict(T=-1), -1), (dict(N=-1), -1), (dict(top=0), -1), (dict(ldd=15), -1),
-                     (dict(ldy=15), -1), (dict(out_flags=2), -1), (dict(T=1 << 30, top=4), -1), (dict(D=A + 1), -2),
-                     (dict(Y=A + 1), -2), (dict(T=1 << 24, N=1 << 20, ldd=1 << 20, ldy=1 << 20), -1)):
+                     (dict(ldy=15), -1), (dict(out_flags=2), -1), (dict(T=1 << 18, top=5), -1), (dict(n=(1 << 20) + 1), -1), (dict(Y=A), -1), (dict(D=A + 1), -2),
+                     (dict(Y=A + 1), -2), (dict(T=1 << 19, N=1 << 20, ldd=1 << 20, ldy=1 << 20), -1)):
         assert S.spense_combine_rows(**{**good, **kw}) == code, kw
     assert S.spense_combine_rows(**{**good, "T": 0}) == 0 and S.spense_combine_rows(**{**good, "N": 0, "Y": None}) == 0
 
@@ -67,11 +69,11 @@ def test_add_adapters_refuses(S):
 
     for kw, code in ((dict(X=None), -1), (dict(order=None), -1), (dict(offsets=None), -1), (dict(base=None), -1),
                      (dict(Y=None), -1), (dict(x_type=3), -1), (dict(base_type=1), -1), (dict(out_flags=4), -1),
-                     (dict(M=-1), -1), (dict(M=1 << 31), -1), (dict(ldx=63), -1), (dict(ldb=47), -1), (dict(ldy=47), -1),
+                     (dict(M=-1), -1), (dict(M=(1 << 20) + 1), -1), (dict(ldx=63), -1), (dict(ldb=47), -1), (dict(ldy=47), -1),
                      (dict(X=A + 2), -2), (dict(ldx=68), -2), (dict(base=A + 2), -2), (dict(Y=A + 1), -2),
                      (dict(Y=A), -1),  # base in the place of Y, of another type
                      (dict(Y=A, out_flags=1, ldy=64), -1), (dict(ws=None), -4), (dict(ws_bytes=0), -4),
-                     (dict(ws=A + 8), -2), (dict(M=1 << 25), -1)):
+                     (dict(ws=A + 8), -2)):
         assert call(**kw) == code, kw
     for kw, code in ((dict(count=0), -1), (dict(count=1025), -1), (dict(R=0), -1), (dict(R=12), -1), (dict(R=136), -1),
                      (dict(K=0), -1), (dict(N=0), -1), (dict(K=48), -2), (dict(A=None), -1), (dict(B=None), -1),
@@ -79,6 +81,8 @@ def test_add_adapters_refuses(S):
         assert call(kw, ldx=max(64, kw.get("K", 64))) == code, kw
         if "A" not in kw and "B" not in kw and kw.get("K") != 1 << 27:
             assert S.spense_adapters_workspace_size(8, pool(S, **kw)) == 0
+    big = dict(M=1 << 20, ldb=1 << 21, ldy=1 << 21, ws_bytes=1 << 40)
+    assert call(dict(N=1 << 21), **big) == -1 and "grid" in S.spense_last_error()
     assert S._lib.spense_add_adapters(A, 2, 8, 64, None, A, A, None, A, 3, 48, A, 48, 0, A, 1 << 20, None) == -1
     assert call(M=0) == 0 and S.spense_adapters_workspace_size(0, pool(S)) == 0
     need = S.spense_adapters_workspace_size(8, pool(S))
@@ -114,7 +118,8 @@ def test_gemm_experts_refuses(S):
                  ldy_array=(ctypes.c_int64 * len(ldy))(*ldy), out_flags=0, stream=None)
         return S.spense_gemm_experts(**{**a, **kw})
 
-    for kw, code in ((dict(X=None), -1), (dict(offsets=None), -1), (dict(rows_x=-1), -1), (dict(n=-1), -1), (dict(n=1 << 31), -1),
+    for kw, code in ((dict(X=None), -1), (dict(offsets=None), -1), (dict(rows_x=-1), -1), (dict(n=-1), -1),
+                     (dict(n=(1 << 20) + 1), -1),
                      (dict(top=0), -1), (dict(count=0), -1), (dict(count=1025), -1), (dict(weights=0), -1), (dict(weights=3), -1),
                      (dict(packed_array=None), -1), (dict(Y_array=None), -1), (dict(ldy_array=None), -1), (dict(out_flags=2), -1),
                      (dict(ldx=127), -1), (dict(ldx=136), -2), (dict(X=A + 8), -2), (dict(Y=(None,)), -1), (dict(Y=(A + 1,)), -2),
@@ -128,4 +133,48 @@ def test_gemm_experts_refuses(S):
     two = dict(Y=(2 * A, 4 * A), ldy=(64, 64))
     for bad in (dict(N=80), dict(K=160), dict(dense_begin=48), dict(split=1)):
         assert call([desc(), desc(**bad)], **two) == -1, bad
+    assert call([desc(), desc()], Y=(2 * A, 2 * A), ldy=(64, 64)) == -1
+    wide = dict(N=1 << 20, dense_begin=0, values=None, meta=None, K=512, dense_ld=512)
+    assert call([desc(**wide)], n=1 << 20, ldy=(1 << 20,), ldx=512) == -1 and "grid" in S.spense_last_error()
     assert call(n=0, X=None) == 0
+
+
+def test_gemm_experts_glu_refuses(S):
+    import ctypes
+
+    def desc(**kw):
+        d = dict(dtype=1, split=0, N=64, K=128, dense_begin=32, values=A, values_ld=64, meta=A, meta_ld=4, dense=A,
+                 dense_ld=128, layout=1)
+        return S.spense_packed_t(**{**d, **kw})
+
+    size = S.spense_gemm_experts_glu_fp8_workspace_size
+
+    def call(gate={}, up={}, **kw):
+        a = dict(X=A, rows_x=8, ldx=128, x_scale=None, order=A, top=1, offsets=A, n=8, count=4,
+                 gate=None if gate is None else ctypes.byref(desc(**gate)),
+                 up=None if up is None else ctypes.byref(desc(**up)), w_scale_gate=None, w_scale_up=None, q=A, ldq=64,
+                 scales=A, ws=A, ws_bytes=size(8, 4, 64), stream=None)
+        return S._lib.spense_gemm_experts_glu_fp8(*{**a, **kw}.values())
+
+    for kw, code in ((dict(X=None), -1), (dict(offsets=None), -1), (dict(rows_x=-1), -1), (dict(n=-1), -1),
+                     (dict(n=(1 << 20) + 1), -1), (dict(top=0), -1), (dict(count=0), -1), (dict(count=1025), -1),
+                     (dict(gate=None), -1), (dict(up=None), -1), (dict(ldx=127), -1), (dict(ldx=136), -2), (dict(X=A + 8), -2),
+                     (dict(q=None), -1), (dict(scales=None), -1), (dict(ldq=63), -1), (dict(ws=None), -4),
+                     (dict(ws_bytes=size(8, 4, 64) - 1), -4), (dict(ws=A + 128), -2)):
+        assert call(**kw) == code, kw
+        assert S.spense_last_error()
+    for bad in (dict(N=80), dict(K=160), dict(dense_begin=48), dict(split=1), dict(dtype=2), dict(layout=0)):
+        assert call(up=bad) == -1, bad
+    assert call(gate=dict(split=1), up=dict(split=1)) == -1
+    assert call(n=0, X=None, q=None, ws=None) == 0 and S.spense_last_error() == ""
+
+
+def test_glu_workspace_size(S):
+    """fp32 G and U, or H and its maxima, of every row; 0 for sizes that the call refuses."""
+    size = S.spense_gemm_experts_glu_fp8_workspace_size
+    for bad in ((0, 4, 64), (-1, 4, 64), ((1 << 20) + 1, 4, 64), (8, 0, 64), (8, 1025, 64), (8, 4, 0), (8, 4, 1 << 31)):
+        assert size(*bad) == 0, bad
+    for n in (1, 2, 17, 300, 4096, 100000, 1 << 20):
+        for count in (1, 5, 64, 1024):
+            for N in (1, 16, 100, 1536, 25600):
+                assert n * N * 4 < size(n, count, N) <= 2 * (n * (N + 63) * 4 + 256)
