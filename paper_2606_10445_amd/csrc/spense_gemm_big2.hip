@@ -175,12 +175,15 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
     // l % 2 of row l / 2 of the wave's 32
     const int vc = 16 * ((lane & 3) ^ ((lane >> 4) & 3));
     const bool meta_wave = !TL || wave < 4;
+    int at[4], src[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at[i] = m0 + 32 * wave + 8 * i + (lane >> 3);
+    if constexpr (RG) source_rows(er, at, mend, src);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = 32 * wave + 8 * i + (lane >> 3), m = m0 + r;
       if constexpr (RG) {
-        const int src = r < ntok ? source_row(er, m) : -1;
-        xo[i] = src >= 0 ? (uint32_t)src * ldx + (xb ^ (64 * (i & 1))) : kOOB;
+        xo[i] = src[i] >= 0 ? (uint32_t)src[i] * ldx + (xb ^ (64 * (i & 1))) : kOOB;
       } else {
         xo[i] = m < a.M && r < ntok ? (uint32_t)m * ldx + (xb ^ (64 * (i & 1))) : kOOB;
       }
@@ -305,6 +308,12 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
   auto run_dense = [&]() __attribute__((always_inline)) {
     const int xb = 16 * ((lane & 7) ^ (lane >> 4));
     uint32_t lo[8];
+    int at[8], src[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) at[i] = m0 + 64 * w4 + 8 * i + (lane >> 3);
+    if constexpr (RG) {
+      if (!late) source_rows(er, at, mend, src);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (late) {
@@ -316,8 +325,7 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
       } else {
         const int r = 64 * w4 + 8 * i + (lane >> 3), m = m0 + r;
         if constexpr (RG) {
-          const int src = r < ntok ? source_row(er, m) : -1;
-          lo[i] = src >= 0 ? (uint32_t)src * ldx + kbound + (xb ^ (64 * (i & 1))) : kOOB;
+          lo[i] = src[i] >= 0 ? (uint32_t)src[i] * ldx + kbound + (xb ^ (64 * (i & 1))) : kOOB;
         } else {
           lo[i] = m < a.M && r < ntok ? (uint32_t)m * ldx + kbound + (xb ^ (64 * (i & 1))) : kOOB;
         }
@@ -416,7 +424,7 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
     EpiScales<RPW / 2, 1> eu;
     epi_scales(eg, sg, RG ? nullptr : a.sx, a.M, nw, mw, rowend);
     epi_scales(eu, su, nullptr, a.M, nw, mw, rowend);
-    if constexpr (RG) source_scales<NT>(eg.x, er, a.sx, mw, mend);
+    if constexpr (RG) source_rows_scales<NT>(eg.x, er, a.sx, mw, mend);
     if constexpr (RG) barrier_vm_lgkm0<0>();  // the stages are free for H
     // the row block's number over both regions: its two slots of the row maxima
     const int slot = 2 * (R.wg0 / a.tblocks + rb) + wr;
@@ -458,7 +466,7 @@ __device__ __forceinline__ void big2_body(const GemmArgs& a, const ExpertRows& e
   EpiScales<RPW, NT> es;
   const float* const sw_n = RG && MD.sw ? MD.sw + ex * er.N : MD.sw;
   epi_scales(es, sw_n, RG ? nullptr : a.sx, a.M, rblk + 16 * RPW * wr + 4 * lq, mw, rowend);
-  if constexpr (RG) source_scales<NT>(es.x, er, a.sx, mw, mend);
+  if constexpr (RG) source_rows_scales<NT>(es.x, er, a.sx, mw, mend);
   if (!via_lds) {
     void* Y = MD.Y;
     int64_t ldy = MD.ldy;

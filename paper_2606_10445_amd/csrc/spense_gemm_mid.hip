@@ -100,13 +100,16 @@ __device__ __forceinline__ void mid_body(const GemmArgs& a, const ExpertRows& er
     const int xb = 16 * ((lane & 7) ^ (lane >> 4));  // column of this lane's 16 bytes in a step; odd blocks xb ^ 64
     uint32_t xo[XL], vo[2], dof[4], mo = kOOB;  // loop-invariant per-lane offsets, kOOB past M or the region
     int vc = 0;  // row-major values: the byte of this lane's piece inside the step
+    int at[XL], src[XL];
+#pragma unroll
+    for (int i = 0; i < XL; ++i) at[i] = m0 + 8 * (XL * cw + i) + (lane >> 3);
+    if constexpr (RG) source_rows(er, at, mend, src);
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-      const int m = m0 + 8 * (XL * cw + i) + (lane >> 3);
       if constexpr (RG) {
-        const int src = m < mend ? source_row(er, m) : -1;
-        xo[i] = src >= 0 ? (uint32_t)((int64_t)src * a.ldx_b + (xb ^ (64 * (i & 1)))) : kOOB;
+        xo[i] = src[i] >= 0 ? (uint32_t)((int64_t)src[i] * a.ldx_b + (xb ^ (64 * (i & 1)))) : kOOB;
       } else {
+        const int m = at[i];
         xo[i] = m < a.M ? (uint32_t)((int64_t)m * a.ldx_b + (xb ^ (64 * (i & 1)))) : kOOB;
       }
     }
@@ -324,7 +327,7 @@ __device__ __forceinline__ void mid_body(const GemmArgs& a, const ExpertRows& er
   const float* sw = RG && MD.sw ? MD.sw + ex * er.N : MD.sw;
   if (!idle) {
     epi_scales(es, sw, RG ? nullptr : a.sx, a.M, rblk + 16 * RPW * wr + 4 * lq, m0 + 16 * TC * wc + li, rowend);
-    if constexpr (RG) source_scales<TC>(es.x, er, a.sx, m0 + 16 * TC * wc + li, mend);
+    if constexpr (RG) source_rows_scales<TC>(es.x, er, a.sx, m0 + 16 * TC * wc + li, mend);
   }
   if (!via_lds) {
     if (idle) return;

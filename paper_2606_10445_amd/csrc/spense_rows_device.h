@@ -136,6 +136,44 @@ __device__ __forceinline__ void source_scales(float (&x)[CT], const ExpertRows& 
   }
 }
 
+// Both for the tiles of many positions: every entry of order is requested before the first is used, without
+// branches around the loads (16 experts of 1536 x 5120, 256 rows each: gate and up 83.7 -> 79.6 us; where most
+// of a tile is empty, the branches that skip it are faster: 56 rows over 8 experts 29.4 us, without them 30.3).
+// positions p[c] >= 0; -1 from pend on.
+template <int C>
+__device__ __forceinline__ void source_rows(const ExpertRows& er, const int (&p)[C], int pend, int (&src)[C]) {
+  int i[C];
+  unsigned top = 1;
+  if (er.order) {
+    top = (unsigned)er.top;
+#pragma unroll
+    for (int c = 0; c < C; ++c) i[c] = er.order[min(p[c], er.n - 1)];
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; ++c) i[c] = p[c];
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int r = (int)((unsigned)i[c] / top);
+    src[c] = (p[c] < pend) & (i[c] >= 0) & (r < er.rows_x) ? r : -1;
+  }
+}
+
+template <int CT>
+__device__ __forceinline__ void source_rows_scales(float (&x)[CT], const ExpertRows& er, const float* sx, int p, int pend) {
+#pragma unroll
+  for (int c = 0; c < CT; ++c) x[c] = 1.0f;
+  if (!sx || er.rows_x == 0) return;
+  int q[CT], src[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) q[c] = p + 16 * c;
+  source_rows(er, q, pend, src);
+#pragma unroll
+  for (int c = 0; c < CT; ++c) x[c] = sx[max(src[c], 0)];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) x[c] = src[c] >= 0 ? x[c] : 1.0f;
+}
+
 // Most tiles that find_tile can give (host).
 inline int64_t most_tiles(int64_t n, int64_t count, bool rest, int64_t T) {
   const int64_t groups = count + (rest ? 1 : 0);

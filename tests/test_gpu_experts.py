@@ -135,6 +135,35 @@ def test_glu_pair(S, T, top, E, N, K, db, kind):
         assert torch.equal(s[:n], want[1]) and torch.equal(q[:n], want[0])
 
 
+LENGTHS = [0, 1, 63, 64, 65, 128, 129, 191, 192, 193, 255, 256, 257, 319, 320, 321, 384, 385, 448, 449, 512, 513, 576, 577, 0]
+
+
+@pytest.mark.parametrize("E,N,K,split,db", [(25, 700, 96, 0, 304), (100, 200, 64, 1, 32)])
+def test_group_lengths(S, E, N, K, split, db):
+    """Tiles of every length, beginning anywhere; with 100 experts two a lane of the search for a tile."""
+    g = torch.Generator().manual_seed(E)
+    lens = torch.tensor(LENGTHS * 4)[:E][torch.randperm(E, generator=g)]
+    idx = torch.repeat_interleave(torch.arange(E, dtype=torch.int32), lens)
+    idx = torch.cat([idx, torch.full((13,), -1, dtype=torch.int32)])[torch.randperm(int(lens.sum()) + 13, generator=g)]
+    T = idx.numel()
+    (pe, W, sc), (x, xs) = weights(S, g, E, N, K, split, db, True), tokens(g, T, K, True)
+    groups, X = S.group_rows(idx.cuda(), E), x.view(torch.uint8).cuda()
+    order, offsets = groups.order.cpu(), groups.offsets.cpu()
+    assert torch.equal(offsets.diff().long(), lens)
+    for f32 in (False, True):
+        out = torch.full((T, N), 9.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+        S.gemm_experts(X, [pe], groups, [sc.cuda()], xs.cuda(), outs=[out], out_f32=f32)
+        n = check(out.cpu(), order, offsets, x, xs, W, sc, 1, True, f32)
+        assert torch.all(out[n:] == 9)
+    if split == 0:
+        up = weights(S, g, E, N, K, split, db, True)
+        s2 = [sc.cuda() / 64, up[2].cuda()]
+        G, U_ = S.gemm_experts(X, [pe, up[0]], groups, s2, xs.cuda(), out_f32=True)
+        want = S.glu_quantize_fp8(G[:n].contiguous(), U_[:n].contiguous())
+        q, s = S.gemm_experts_glu_fp8(X, pe, up[0], groups, *s2, xs.cuda())
+        assert torch.equal(s[:n], want[1]) and torch.equal(q[:n], want[0])
+
+
 @pytest.mark.parametrize("T,top,E,N,K,split,db", CASES)
 def test_experts_random(S, T, top, E, N, K, split, db):
     g = torch.Generator().manual_seed(T + N + K + 1)
