@@ -213,12 +213,11 @@ __device__ __forceinline__ void store1(float v, uint8_t* row, int n) {
 // over hi of all ranks, then lo: for R <= 16 both in one instruction (lane group q holds eight
 // ranks, block q mod R / 8), else lo in the second half of the KS instructions, on the same
 // fragments of B.  V's fragments stay in LDS: in registers they would leave two waves a SIMD (64
-// tokens, R = 64), too few loads in flight.  A step's B and base are requested before V is
-// there (the first U steps') or U steps ahead, without branches a lane takes by itself.
+// tokens, R = 64), too few loads in flight.  A step's B and base are requested a step ahead, the first
+// step's before V is there, without branches a lane takes by itself.
 template <bool BBF, bool YBF, int KS, int CT>
 __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
-  constexpr int U = CT == 1 ? 2 : 1;             // steps requested together (a.steps is even)
-  constexpr int KB = KS == 1 ? 1 : KS / 2;       // fragments of B
+  constexpr int KB = KS == 1 ? 1 : KS / 2;  // fragments of B
   RowTile t;
   if (!find_tile(a.offsets, a.count, a.M, true, 16 * CT, blockIdx.x / a.nblocks, t)) return;
   const bool none = t.group == a.count;
@@ -236,8 +235,8 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
     row[c] = p < t.p1 ? a.order[p] : -1;
     if (row[c] >= a.M) row[c] = -1;
   }
-  v4i bw[U][2][KB];
-  auto load_b = [&](v4i (&w)[2][KB], int s) {
+  v4i bw[2][KB];
+  auto load_b = [&](int s) {
     const int n0 = n_wg + 32 * (4 * s + wave);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -245,7 +244,7 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
 #pragma unroll
       for (int j = 0; j < KB; ++j) {
         const int b = KS == 1 && lq >= rb ? lq - rb : 4 * j + lq;  // eight ranks
-        w[i][j] = bl16<0>(rw, sel(n < a.N && b < rb, (uint32_t)n * (uint32_t)a.R * 2u + 16u * (uint32_t)b));
+        bw[i][j] = bl16<0>(rw, sel(n < a.N && b < rb, (uint32_t)n * (uint32_t)a.R * 2u + 16u * (uint32_t)b));
       }
     }
   };
@@ -255,92 +254,104 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
   };
   // whole pieces of eight for every lane of the step (the same for all of the wave)
   auto whole = [&](int s) { return n_wg + 32 * (4 * s + wave) + 32 <= a.N; };
-  Eight<BBF> ob[U][CT];
+  Eight<BBF> ob[CT];
+  load_b(0);
+  if (whole(0)) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    load_b(bw[u], u);
-    if (whole(u)) {
-#pragma unroll
-      for (int c = 0; c < CT; ++c) ob[u][c] = load_base(u, c);
-    }
+    for (int c = 0; c < CT; ++c) ob[c] = load_base(0, c);
   }
+  // V of the tile: the slices' sums in order, as fragments of hi and lo.  A wave makes fragment pairs u =
+  // wave, wave + 4, ... (token tile u / KB, ranks of fragment u % KB), all of a slice's loads requested
+  // together; where hi and lo share an instruction one fragment, of which lanes from rb on hold lo.
   {
-    for (int f = wave; f < CT * KS; f += 4) {
-      const int c = f / KS, j = f % KS;
-      const bool lo = KS == 1 ? lq >= rb : j >= KB;
-      const int b = KS == 1 ? (lo ? lq - rb : lq) : 4 * (j % KB) + lq;  // eight ranks
-      const int p = t.p0 + 16 * c + li;
-      v4i w = {0, 0, 0, 0};
-      if (!none && b < rb && p < t.p1) {
-        float v[8];
+    constexpr int PAIRS = CT * KB, PW = (PAIRS + 3) / 4;
+    float v[PW][8];
+    const float* pp[PW];
+    bool in[PW];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-        const float* pp = a.part + (int64_t)p * a.R + 8 * b;
-        const int64_t slice = (int64_t)a.M * a.R;
-#pragma unroll 4
-        for (int s = 0; s < a.slices; ++s) {
+    for (int i = 0; i < PW; ++i) {
+      const int u = wave + 4 * i, c = u / KB, b = KS == 1 && lq >= rb ? lq - rb : 4 * (u % KB) + lq, p = t.p0 + 16 * c + li;
+      in[i] = !none && u < PAIRS && b < rb && p < t.p1;
+      pp[i] = a.part + (in[i] ? (int64_t)p * a.R + 8 * b : 0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+    }
+    const int64_t slice = (int64_t)a.M * a.R;
+    if (!none && wave < PAIRS) {
+#pragma unroll(PW == 1 ? 8 : 2)
+      for (int s = 0; s < a.slices; ++s) {
+#pragma unroll
+        for (int i = 0; i < PW; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const v4f d = *reinterpret_cast<const v4f*>(pp + s * slice + 4 * h);
+            const v4f d = *reinterpret_cast<const v4f*>(pp[i] + s * slice + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * h + e] += d[e];
+            for (int e = 0; e < 4; ++e) v[i][4 * h + e] += d[e];
           }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t hi = bf16_bits(v[e]);
-          const float hf = __uint_as_float(hi << 16);
-          // what hi leaves; nothing where hi is infinite or NaN
-          const uint32_t bits = !lo ? hi : (fabsf(hf) <= 3.3895314e38f ? bf16_bits(v[e] - hf) : 0u);
-          w[e / 2] |= (int)(bits << (16 * (e & 1)));
-        }
       }
-      vfrag[f * 64 + lane] = w;
+    }
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+      const int u = wave + 4 * i, c = u / KB, j = u % KB;
+      if (u >= PAIRS) break;
+      v4i hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t h = bf16_bits(v[i][e]);
+        const float hf = __uint_as_float(h << 16);
+        // what hi leaves; nothing where hi is infinite or NaN
+        const uint32_t l = fabsf(hf) <= 3.3895314e38f ? bf16_bits(v[i][e] - hf) : 0u;
+        hi[e / 2] |= (int)(h << (16 * (e & 1)));
+        lo[e / 2] |= (int)(l << (16 * (e & 1)));
+      }
+      if (!in[i]) hi = lo = (v4i){0, 0, 0, 0};
+      if constexpr (KS == 1) {
+        vfrag[c * 64 + lane] = lq >= rb ? lo : hi;
+      } else {
+        vfrag[(c * KS + j) * 64 + lane] = hi;
+        vfrag[(c * KS + j + KB) * 64 + lane] = lo;
+      }
     }
     __syncthreads();
   }
-  for (int s0 = 0; s0 < a.steps; s0 += U) {
+  for (int s = 0; s < a.steps; ++s) {
+    const int n0 = n_wg + 32 * (4 * s + wave), nq = n0 + 8 * lq;
+    if (n0 >= a.N) return;
+    const bool full = whole(s);
+    v4f acc[CT][2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s = s0 + u;
-      const int n0 = n_wg + 32 * (4 * s + wave), nq = n0 + 8 * lq;
-      if (n0 >= a.N) return;
-      const bool full = whole(s);
-      v4f acc[CT][2];
+    for (int c = 0; c < CT; ++c) {
+      acc[c][0] = acc[c][1] = (v4f){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        acc[c][0] = acc[c][1] = (v4f){0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < KS; ++j) {
+        const v4i vf = vfrag[(c * KS + j) * 64 + lane];
 #pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          const v4i vf = vfrag[(c * KS + j) * 64 + lane];
+        for (int i = 0; i < 2; ++i) acc[c][i] = mma_bf16(bw[i][j % KB], vf, acc[c][i]);
+      }
+    }
+    xdl_fence();
+    if (s + 1 < a.steps) load_b(s + 1);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) acc[c][i] = mma_bf16(bw[u][i][j % KB], vf, acc[c][i]);
+    for (int c = 0; c < CT; ++c) {
+      uint8_t* yr = a.Y + (int64_t)row[c] * a.ldy_b;
+      if (full) {
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = none ? value<BBF>(ob[c], e) : value<BBF>(ob[c], e) + acc[c][e / 4][e % 4];
+        if (row[c] >= 0) store8<YBF>(o, yr, nq);
+      } else if (row[c] >= 0) {  // the ragged end of N
+        const uint8_t* br = a.base + (int64_t)row[c] * a.ldb_b;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (nq + e >= a.N) continue;
+          const float o = load1<BBF>(br, nq + e);
+          store1<YBF>(none ? o : o + acc[c][e / 4][e % 4], yr, nq + e);
         }
       }
-      xdl_fence();
-      if (s0 + U < a.steps) load_b(bw[u], s + U);
+    }
+    if (s + 1 < a.steps && whole(s + 1)) {
 #pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        uint8_t* yr = a.Y + (int64_t)row[c] * a.ldy_b;
-        if (full) {
-          float o[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = none ? value<BBF>(ob[u][c], e) : value<BBF>(ob[u][c], e) + acc[c][e / 4][e % 4];
-          if (row[c] >= 0) store8<YBF>(o, yr, nq);
-        } else if (row[c] >= 0) {  // the ragged end of N
-          const uint8_t* br = a.base + (int64_t)row[c] * a.ldb_b;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (nq + e >= a.N) continue;
-            const float o = load1<BBF>(br, nq + e);
-            store1<YBF>(none ? o : o + acc[c][e / 4][e % 4], yr, nq + e);
-          }
-        }
-      }
-      if (s0 + U < a.steps && whole(s + U)) {
-#pragma unroll
-        for (int c = 0; c < CT; ++c) ob[u][c] = load_base(s + U, c);
-      }
+      for (int c = 0; c < CT; ++c) ob[c] = load_base(s + 1, c);
     }
   }
 }
@@ -352,14 +363,15 @@ bool many_tokens(int64_t M, int32_t count, int32_t R) { return R <= 64 && M >= 3
 int shrink_tokens(int64_t M, int32_t count, int32_t R) { return many_tokens(M, count, R) ? 32 : 16; }
 int expand_tokens(int64_t M, int32_t count, int32_t R) { return many_tokens(M, count, R) ? 64 : 16; }
 
-// K slices: workgroups for the CUs, each with two rounds of steps or more; but every slice is another
-// M x R of partial sums, which each workgroup along N of the second launch reads again.  us at 2 / 4 / 8
-// slices: M = 2048, R = 64, N = 8192 55 / 63 / 71 (80 workgroups a slice), M = 1000, R = 32, N = 16384
-// 35 / 31 / 35 (35); at 8 / 16, M = 64, R = 16, N = 25600 16.8 / 17.3, M = 256, N = 8192 11.8 / 12.8.
+// K slices: a workgroup for every CU (two where tiles are of 16 tokens, each with two rounds of steps or
+// more); but every slice is another M x R of partial sums, which each workgroup along N of the second
+// launch reads again.  us (both launches and the grouping): M = 2048, R = 64, N = 8192, 80 tiles, 2 / 4
+// slices 53.7 / 48.5; M = 4096, R = 64, 132 tiles, 2 / 4 39.0 / 44.5; M = 1000, R = 32, N = 16384, 40 tiles, 4 / 8
+// 39.1 / 42.4; tiles of 16 at 8 / 16: M = 64, R = 16, N = 25600 16.8 / 17.3, M = 256, N = 8192 11.8 / 12.8.
 int k_slices(int64_t M, int32_t count, int64_t K, int32_t R) {
   const bool many = many_tokens(M, count, R);
   const int64_t wg = most_tiles(M, count, false, shrink_tokens(M, count, R)) * ((R + 63) / 64);
-  int64_t s = ((many ? 160 : 512) + wg - 1) / wg;
+  int64_t s = ((many ? 256 : 512) + wg - 1) / wg;
   const int64_t cap = many ? 4 : 8, most = (K + 511) / 512;
   s = s < most ? s : most;
   s = s < cap ? s : cap;
