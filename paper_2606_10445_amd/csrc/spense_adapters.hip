@@ -212,8 +212,7 @@ __device__ __forceinline__ void store1(float v, uint8_t* row, int n) {
 // with eight consecutive outputs, columns 8 q .. 8 q + 7 of the 32.  The product's k index runs
 // over hi of all ranks, then lo: for R <= 16 both in one instruction (lane group q holds eight
 // ranks, block q mod R / 8), else lo in the second half of the KS instructions, on the same
-// fragments of B.  V's fragments stay in LDS: in registers they would leave two waves a SIMD (64
-// tokens, R = 64), too few loads in flight.  A step's B and base are requested a step ahead, the first
+// fragments of B.  V's fragments stay in LDS, whose reads hide behind the loads.  A step's B and base are requested a step ahead, the first
 // step's before V is there, without branches a lane takes by itself.
 template <bool BBF, bool YBF, int KS, int CT>
 __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
@@ -356,12 +355,11 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
   }
 }
 
-// Tokens of a tile: 64 (32 in the first launch, whose K leaves more to do per token) where the batch
-// holds many tokens per adapter, so that A and B rows feed several matrix instructions a load; 16
-// where it does not (a tile holds one adapter's tokens).
-bool many_tokens(int64_t M, int32_t count, int32_t R) { return R <= 64 && M >= 32 * (int64_t)count && M >= 128; }
-int shrink_tokens(int64_t M, int32_t count, int32_t R) { return many_tokens(M, count, R) ? 32 : 16; }
-int expand_tokens(int64_t M, int32_t count, int32_t R) { return many_tokens(M, count, R) ? 64 : 16; }
+// Tokens of a tile: 32 where the batch holds many tokens per adapter, so that A and B rows feed several
+// matrix instructions a load; 16 where it does not (a tile holds one adapter's tokens).  64 in the second
+// launch: M = 2048 in runs of 150, R = 64 49.7 us against 51.0, but M = 1000, R = 32 in runs of 100 40.8
+// against 39.2 and M = 500, R = 64 in runs of 70 30.0 against 25.8.
+int tile_tokens(int64_t M, int32_t count, int32_t R) { return R <= 64 && M >= 32 * (int64_t)count && M >= 128 ? 32 : 16; }
 
 // K slices: a workgroup for every CU (two where tiles are of 16 tokens, each with two rounds of steps or
 // more); but every slice is another M x R of partial sums, which each workgroup along N of the second
@@ -369,8 +367,9 @@ int expand_tokens(int64_t M, int32_t count, int32_t R) { return many_tokens(M, c
 // slices 53.7 / 48.5; M = 4096, R = 64, 132 tiles, 2 / 4 39.0 / 44.5; M = 1000, R = 32, N = 16384, 40 tiles, 4 / 8
 // 39.1 / 42.4; tiles of 16 at 8 / 16: M = 64, R = 16, N = 25600 16.8 / 17.3, M = 256, N = 8192 11.8 / 12.8.
 int k_slices(int64_t M, int32_t count, int64_t K, int32_t R) {
-  const bool many = many_tokens(M, count, R);
-  const int64_t wg = most_tiles(M, count, false, shrink_tokens(M, count, R)) * ((R + 63) / 64);
+  const int T = tile_tokens(M, count, R);
+  const bool many = T == 32;
+  const int64_t wg = most_tiles(M, count, false, T) * ((R + 63) / 64);
   int64_t s = ((many ? 256 : 512) + wg - 1) / wg;
   const int64_t cap = many ? 4 : 8, most = (K + 511) / 512;
   s = s < most ? s : most;
@@ -398,13 +397,13 @@ template <bool BBF, bool YBF>
 void launch_expand(const AdapterArgs& a, int T, int64_t tiles, hipStream_t st) {
   const dim3 grid((unsigned)(tiles * a.nblocks));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
-  if (T == 64) {
+  if (T == 32) {
     if (a.R <= 16)
-      go(adapter_expand_kernel<BBF, YBF, 1, 4>);
+      go(adapter_expand_kernel<BBF, YBF, 1, 2>);
     else if (a.R <= 32)
-      go(adapter_expand_kernel<BBF, YBF, 2, 4>);
+      go(adapter_expand_kernel<BBF, YBF, 2, 2>);
     else
-      go(adapter_expand_kernel<BBF, YBF, 4, 4>);
+      go(adapter_expand_kernel<BBF, YBF, 4, 2>);
   } else {
     if (a.R <= 16)
       go(adapter_expand_kernel<BBF, YBF, 1, 1>);
@@ -467,14 +466,14 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   const int64_t xb = ((M - 1) * ldx + P.K) * xs;
   if (xb >= lim) return api_fail(SPENSE_ERR_ARG, "X spans 2 GiB or more");
   if (P.K * P.R * 2 >= lim || P.N * P.R * 2 >= lim) return api_fail(SPENSE_ERR_ARG, "an adapter spans 2 GiB or more");
-  const int T = spense::expand_tokens(M, P.count, P.R), Ts = spense::shrink_tokens(M, P.count, P.R);
-  const int64_t tiles = spense::most_tiles(M, P.count, false, Ts), all_tiles = spense::most_tiles(M, P.count, true, T);
-  // columns a workgroup: as many of 1024 (tiles of 16), 512 or 256 as leave workgroups enough, their
-  // start (the tile, V) then paid less often.  us at 256 / 512 / 1024: M = 64 over 28 adapters, N =
-  // 25600 18.9 / 17.3 / 15.4; M = 1 7.9 / 8.6 / 10.0, M = 128 over 8, N = 8192 9.6 / 10.3 / 12.6; M =
-  // 2048, N = 8192 in tiles of 64 55.6 / 52.3 / 58.9.
-  const int64_t used = P.count < M ? P.count : M, tiles_used = T == 64 ? M / 64 + used / 2 : used;
-  int steps = T == 64 ? 4 : 8;
+  const int T = spense::tile_tokens(M, P.count, P.R);
+  const int64_t tiles = spense::most_tiles(M, P.count, false, T), all_tiles = spense::most_tiles(M, P.count, true, T);
+  // columns a workgroup: as many of 1024, 512 or 256 as leave workgroups enough, their start (the tile, V)
+  // then paid less often.  us at 256 / 512 / 1024: M = 64 over 28 adapters, N = 25600 18.9 / 17.3 / 15.4;
+  // M = 1 7.9 / 8.6 / 10.0, M = 128 over 8, N = 8192 9.6 / 10.3 / 12.6; M = 2048, N = 8192 51.2 / 51.2 / 50.2
+  // with the grouping.
+  const int64_t used = P.count < M ? P.count : M, tiles_used = T == 32 ? M / 32 + used / 2 : used;
+  int steps = 8;
   while (steps > 2 && tiles_used * ((P.N + 128 * steps - 1) / (128 * steps)) < 512) steps /= 2;
   const int64_t nblocks = (P.N + 128 * steps - 1) / (128 * steps);
   if (!spense::grid_fits(all_tiles * nblocks, 256)) return api_fail(SPENSE_ERR_ARG, "M x N too large for the grid");
@@ -497,9 +496,9 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   a.nblocks = (int32_t)nblocks;
   a.steps = steps;
   if (x_type == SPENSE_FP8_E4M3FN)
-    Ts == 32 ? spense::launch_shrink<true, 2>(a, tiles, stream) : spense::launch_shrink<true, 1>(a, tiles, stream);
+    T == 32 ? spense::launch_shrink<true, 2>(a, tiles, stream) : spense::launch_shrink<true, 1>(a, tiles, stream);
   else
-    Ts == 32 ? spense::launch_shrink<false, 2>(a, tiles, stream) : spense::launch_shrink<false, 1>(a, tiles, stream);
+    T == 32 ? spense::launch_shrink<false, 2>(a, tiles, stream) : spense::launch_shrink<false, 1>(a, tiles, stream);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) {
     if (bs == 2)
