@@ -905,14 +905,20 @@ def _on_gpu(dev, *tensors):
 
 
 def _rows_of(t, name, shape, dtype=None):
-    """A 2-D tensor of this shape with contiguous rows that do not overlap."""
-    _row_major(t, name)
-    if tuple(t.shape) != tuple(shape):
+    """Checks for a 2-D tensor of this shape with contiguous rows that do not overlap; returns its
+    leading dimension."""
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-        raise ValueError(f"{name}'s rows overlap")
+    ld, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{name} must be a 2-D row-major tensor")
+    if ld < shape[1]:
+        if shape[0] > 1:
+            raise ValueError(f"{name}'s rows overlap")
+        ld = shape[1]  # a single row's stride does not matter
+    return ld
 
 
 def _ld(t):
@@ -939,63 +945,61 @@ def block_norm(x: torch.Tensor, y: torch.Tensor | None = None, *, post_weight=No
     residual_out may be x and normed_out may be y."""
     if x.dim() != 2:
         raise ValueError("x must be a 2-D row-major tensor")
-    M, K = x.shape
-    _rows_of(x, "x", (M, K))
-    dev = x.device
+    shape = M, K = tuple(x.shape)
+    ldx, dev, xdtype = _rows_of(x, "x", shape), x.device, x.dtype
     xt = _act_type(x)
+    ldy = ldg = ldr = ldn = ldq = 0
     if y is None:
         if gate is not None or post_weight is not None:
             raise ValueError("gate and post_weight need a block output y")
-        yt, ydtype = xt, x.dtype
+        if residual_out is not None:
+            raise ValueError("without y there is no new residual")
+        yt, ydtype = xt, xdtype
     else:
-        _rows_of(y, "y", (M, K))
+        ldy = _rows_of(y, "y", shape)
         yt, ydtype = _act_type(y), y.dtype
-    ldg = 0
     if gate is not None:
         if gate.dtype != ydtype:
             raise ValueError(f"gate is {gate.dtype}, expected {ydtype}")
         if gate.dim() == 1:
             if gate.shape[0] != K or not gate.is_contiguous():
-                raise ValueError(f"gate must be a contiguous vector of length {K} or of shape {(M, K)}")
+                raise ValueError(f"gate must be a contiguous vector of length {K} or of shape {shape}")
         else:
-            _rows_of(gate, "gate", (M, K))
-            ldg = _ld(gate)
+            ldg = _rows_of(gate, "gate", shape)
     wt = None
     for w, name in ((post_weight, "post_weight"), (weight, "weight")):
         if w is None:
             continue
-        if w.dim() != 1 or w.shape[0] != K or not w.is_contiguous():
+        if w.shape != (K,) or not w.is_contiguous():
             raise ValueError(f"{name} must be a contiguous vector of length {K}")
         if wt is not None and _act_type(w) != wt:
             raise ValueError("post_weight and weight must have one type")
         wt = _act_type(w)
-    normed = normed or normed_out is not None
-    quantize = quantize or codes_out is not None or scales_out is not None
-    if y is None and residual_out is not None:
-        raise ValueError("without y there is no new residual")
     _on_gpu(dev, y, gate, post_weight, weight, residual_out, normed_out, codes_out, scales_out)
-    r = n = q = s = None
+    r, n, q, s = residual_out, normed_out, codes_out, scales_out
     if y is not None:
-        if residual_out is not None:
-            _rows_of(residual_out, "residual_out", (M, K), x.dtype)
-        r = torch.empty((M, K), dtype=x.dtype, device=dev) if residual_out is None else residual_out
-    if normed:
-        if normed_out is not None:
-            _rows_of(normed_out, "normed_out", (M, K), ydtype)
-        n = torch.empty((M, K), dtype=ydtype, device=dev) if normed_out is None else normed_out
-    if quantize:
-        if codes_out is not None:
-            _rows_of(codes_out, "codes_out", (M, K), torch.uint8)
-        if scales_out is not None:
-            _check_scale(scales_out, M, dev, "scales_out")
-        q = torch.empty((M, K), dtype=torch.uint8, device=dev) if codes_out is None else codes_out
-        s = torch.empty(M, dtype=torch.float32, device=dev) if scales_out is None else scales_out
+        if r is None:
+            r, ldr = torch.empty(shape, dtype=xdtype, device=dev), K
+        else:
+            ldr = _rows_of(r, "residual_out", shape, xdtype)
+    if n is not None:
+        ldn = _rows_of(n, "normed_out", shape, ydtype)
+    elif normed:
+        n, ldn = torch.empty(shape, dtype=ydtype, device=dev), K
+    if quantize or q is not None or s is not None:
+        if q is None:
+            q, ldq = torch.empty(shape, dtype=torch.uint8, device=dev), K
+        else:
+            ldq = _rows_of(q, "codes_out", shape, torch.uint8)
+        if s is None:
+            s = torch.empty(M, dtype=torch.float32, device=dev)
+        else:
+            _check_scale(s, M, dev, "scales_out")
     if r is None and n is None and q is None:
         raise ValueError("no output is asked for")
-    a = spense_block_norm_t(M, K, _ptr(x), _ld(x), xt, yt, _ptr(y), 0 if y is None else _ld(y), _ptr(gate), ldg,
-                            _ptr(post_weight), _ptr(weight), wt or SPENSE_F32, residual_scale, eps, _ptr(r),
-                            0 if r is None else _ld(r), _ptr(n), 0 if n is None else _ld(n), _ptr(q),
-                            0 if q is None else _ld(q), _ptr(s))
+    a = spense_block_norm_t(M, K, x.data_ptr(), ldx, xt, yt, _ptr(y), ldy, _ptr(gate), ldg, _ptr(post_weight),
+                            _ptr(weight), wt or SPENSE_F32, residual_scale, eps, _ptr(r), ldr, _ptr(n), ldn, _ptr(q), ldq,
+                            _ptr(s))
     with _device(dev):
         _check(spense_block_norm(a, _stream(dev)))
     return BlockNorm(r, n, q, s)
@@ -1052,7 +1056,7 @@ def combine_rows(D: torch.Tensor, groups: RowGroups, weights: torch.Tensor | Non
     if D.dim() != 2:
         raise ValueError("D must be a 2-D row-major tensor")
     n, N = D.shape
-    _rows_of(D, "D", (n, N))
+    ldd = _rows_of(D, "D", (n, N))
     if top < 1 or groups.n != n or n % top:
         raise ValueError(f"D has {n} rows, the groups {groups.n}; both must be T * top with top = {top}")
     T = n // top
@@ -1063,7 +1067,7 @@ def combine_rows(D: torch.Tensor, groups: RowGroups, weights: torch.Tensor | Non
         raise ValueError(f"weights must be a contiguous fp32 tensor of {n} entries")
     out = _out(out, T, N, out_f32, dev)
     with _device(dev):
-        _check(spense_combine_rows(_ptr(D), _act_type(D), n, _ld(D), groups.inverse_ptr, _ptr(weights), T, top, N,
+        _check(spense_combine_rows(_ptr(D), _act_type(D), n, ldd, groups.inverse_ptr, _ptr(weights), T, top, N,
                                    _ptr(out), _ld(out), SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, _stream(dev)))
     return out
 
@@ -1096,25 +1100,27 @@ def add_adapters(base: torch.Tensor, X: torch.Tensor, pool: AdapterPool, groups:
     base: M x N, bf16 or fp32, the projection's output; X: M x K, bf16 or fp8 codes with x_scale;
     groups: group_rows of the tokens' adapter indices over pool.count groups (tokens of no group get
     base).  out may be base."""
-    M = X.shape[0]
-    _rows_of(X, "X", (M, pool.K))
-    dev = X.device
-    xt = SPENSE_BF16 if X.dtype == torch.bfloat16 else _act_code(X)
-    if xt is None or X.dtype in (torch.int16, torch.uint16):
-        raise ValueError(f"X is {X.dtype}; adapters take fp8 codes (uint8) or bfloat16")
-    _rows_of(base, "base", (M, pool.N))
+    M, N, dev, xd = X.shape[0], pool.N, X.device, X.dtype
+    ldx, ldb = _rows_of(X, "X", (M, pool.K)), _rows_of(base, "base", (M, N))
+    xt = SPENSE_BF16 if xd == torch.bfloat16 else _act_code(X)
+    if xt is None or xd in (torch.int16, torch.uint16):
+        raise ValueError(f"X is {xd}; adapters take fp8 codes (uint8) or bfloat16")
     bt = _act_type(base)
     if groups.n != M or groups.groups != pool.count:
         raise ValueError(f"groups are of {groups.n} rows over {groups.groups}, expected {M} over {pool.count}")
     _on_gpu(dev, base, pool.A)
     _same_device(groups, dev)
     _check_scale(x_scale, M, dev, "x_scale")
-    out = _out(out, M, pool.N, out_f32, dev)
+    if out is None:
+        out, ldy = torch.empty((M, N), dtype=torch.float32 if out_f32 else torch.bfloat16, device=dev), N
+    else:
+        out = _out(out, M, N, out_f32, dev)
+        ldy = _ld(out)
     ws = workspace or _CallScratch(dev)
     with _device(dev):
         wp, wn = ws.get(spense_adapters_workspace_size(M, pool.desc))
-        _check(spense_add_adapters(_ptr(X), xt, M, _ld(X), _ptr(x_scale), groups.order_ptr, groups.offsets_ptr,
-                                   pool.desc, _ptr(base), bt, _ld(base), _ptr(out), _ld(out),
+        _check(spense_add_adapters(X.data_ptr(), xt, M, ldx, _ptr(x_scale), groups.order_ptr, groups.offsets_ptr, pool.desc,
+                                   base.data_ptr(), bt, ldb, out.data_ptr(), ldy,
                                    SPENSE_OUT_F32 if out_f32 else SPENSE_OUT_BF16, wp, wn, _stream(dev)))
     return out
 
