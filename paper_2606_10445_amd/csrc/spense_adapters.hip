@@ -212,8 +212,9 @@ __device__ __forceinline__ void store1(float v, uint8_t* row, int n) {
 // with eight consecutive outputs, columns 8 q .. 8 q + 7 of the 32.  The product's k index runs
 // over hi of all ranks, then lo: for R <= 16 both in one instruction (lane group q holds eight
 // ranks, block q mod R / 8), else lo in the second half of the KS instructions, on the same
-// fragments of B.  V's fragments stay in LDS, whose reads hide behind the loads.  A step's B and base are requested a step ahead, the first
-// step's before V is there, without branches a lane takes by itself.
+// fragments of B.  V's fragments stay in LDS, whose reads hide behind the loads.  A step's B and base are
+// requested a step ahead, the first step's before V is there, without branches a lane takes by itself
+// (base two steps ahead: no faster).
 template <bool BBF, bool YBF, int KS, int CT>
 __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
   constexpr int KB = KS == 1 ? 1 : KS / 2;  // fragments of B
@@ -357,14 +358,14 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
 
 // Tokens of a tile: 32 where the batch holds many tokens per adapter, so that A and B rows feed several
 // matrix instructions a load; 16 where it does not (a tile holds one adapter's tokens).  64 in the second
-// launch: M = 2048 in runs of 150, R = 64 49.7 us against 51.0, but M = 1000, R = 32 in runs of 100 40.8
-// against 39.2 and M = 500, R = 64 in runs of 70 30.0 against 25.8.
+// launch: M = 2048 in runs of 150, R = 64 52.3 us against 52.6, M = 1000, R = 32, N = 16384 in runs of 100 43.4
+// against 44.7, but M = 500, R = 64 in runs of 70 30.0 against 25.6.
 int tile_tokens(int64_t M, int32_t count, int32_t R) { return R <= 64 && M >= 32 * (int64_t)count && M >= 128 ? 32 : 16; }
 
 // K slices: a workgroup for every CU (two where tiles are of 16 tokens, each with two rounds of steps or
 // more); but every slice is another M x R of partial sums, which each workgroup along N of the second
 // launch reads again.  us (both launches and the grouping): M = 2048, R = 64, N = 8192, 80 tiles, 2 / 4
-// slices 53.7 / 48.5; M = 4096, R = 64, 132 tiles, 2 / 4 39.0 / 44.5; M = 1000, R = 32, N = 16384, 40 tiles, 4 / 8
+// slices 60.5 / 54.7; M = 4096, R = 64, 132 tiles, 2 / 4 39.0 / 44.5; M = 1000, R = 32, N = 16384, 40 tiles, 4 / 8
 // 39.1 / 42.4; tiles of 16 at 8 / 16: M = 64, R = 16, N = 25600 16.8 / 17.3, M = 256, N = 8192 11.8 / 12.8.
 int k_slices(int64_t M, int32_t count, int64_t K, int32_t R) {
   const int T = tile_tokens(M, count, R);
@@ -468,12 +469,12 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   if (P.K * P.R * 2 >= lim || P.N * P.R * 2 >= lim) return api_fail(SPENSE_ERR_ARG, "an adapter spans 2 GiB or more");
   const int T = spense::tile_tokens(M, P.count, P.R);
   const int64_t tiles = spense::most_tiles(M, P.count, false, T), all_tiles = spense::most_tiles(M, P.count, true, T);
-  // columns a workgroup: as many of 1024, 512 or 256 as leave workgroups enough, their start (the tile, V)
-  // then paid less often.  us at 256 / 512 / 1024: M = 64 over 28 adapters, N = 25600 18.9 / 17.3 / 15.4;
-  // M = 1 7.9 / 8.6 / 10.0, M = 128 over 8, N = 8192 9.6 / 10.3 / 12.6; M = 2048, N = 8192 51.2 / 51.2 / 50.2
-  // with the grouping.
+  // columns a workgroup: as many of 1024 (512 with tiles of 32), 512 or 256 as leave workgroups enough,
+  // their start (the tile, V) then paid less often.  us at 256 / 512 / 1024: M = 64 over 28 adapters, N = 25600
+  // 18.9 / 17.3 / 15.4; M = 1 7.9 / 8.6 / 10.0, M = 128 over 8, N = 8192 9.6 / 10.3 / 12.6; M = 2048, N = 8192
+  // with the grouping 53.8 / 52.6 / 54.7.
   const int64_t used = P.count < M ? P.count : M, tiles_used = T == 32 ? M / 32 + used / 2 : used;
-  int steps = 8;
+  int steps = T == 32 ? 4 : 8;
   while (steps > 2 && tiles_used * ((P.N + 128 * steps - 1) / (128 * steps)) < 512) steps /= 2;
   const int64_t nblocks = (P.N + 128 * steps - 1) / (128 * steps);
   if (!spense::grid_fits(all_tiles * nblocks, 256)) return api_fail(SPENSE_ERR_ARG, "M x N too large for the grid");
