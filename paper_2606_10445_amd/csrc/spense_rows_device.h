@@ -136,10 +136,10 @@ __device__ __forceinline__ void source_scales(float (&x)[CT], const ExpertRows& 
   }
 }
 
-// Both for the tiles of many positions: every entry of order is requested before the first is used, without
-// branches around the loads (16 experts of 1536 x 5120, 256 rows each: gate and up 83.7 -> 79.6 us; where most
-// of a tile is empty, the branches that skip it are faster: 56 rows over 8 experts 29.4 us, without them 30.3).
-// positions p[c] >= 0; -1 from pend on.
+// The same two for tiles of many positions (p[c] >= 0; -1 from pend on): every entry of order is requested
+// before the first is used, without branches around the loads.  Gate and up of 16 experts of 1536 x 5120, 256
+// rows each 83.7 -> 79.6 us; where most of a tile is empty the branches that skip it are faster: 56 rows over
+// 8 experts 29.4 us against 30.3.
 template <int C>
 __device__ __forceinline__ void source_rows(const ExpertRows& er, const int (&p)[C], int pend, int (&src)[C]) {
   int i[C];
