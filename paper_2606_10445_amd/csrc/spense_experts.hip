@@ -457,7 +457,13 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
   const int64_t most = spense::most_tiles(c.er.n, c.er.count, false, 16 * ct);
   const int64_t lds = stream_lds(chunks, ct);
   const bool stream_kernel = streams(chunks, ct);
-  const int wv = ct == 1 ? 4 : 8;
+  const int64_t used = c.er.count < c.er.n ? c.er.count : c.er.n, tiles_even = used * ceil_div(c.er.n / used, 16 * ct);
+  // Waves a workgroup: eight for wider tiles, four for tiles of 16, or two of them where the fullest CU, of up to
+  // 12 waves, then gets fewer.  us at four / two, gate and up of one token's experts: 1 of 1536 x 5120 13.8 / 11.4, 2 14.5 /
+  // 11.8, 6 22.4 / 20.1, 8 23.4 / 21.5; as many waves either way: 4 15.6 / 15.9, 10 25.0 / 25.4, 64 experts 99.9
+  // / 103.3.
+  auto fullest = [&](int64_t w) { return w * ceil_div(tiles_even * ceil_div(tiles, w), 256); };
+  const int wv = ct > 1 ? 8 : !stream_kernel && fullest(4) <= 12 && fullest(2) < fullest(4) ? 2 : 4;
   if (stream_kernel) {
     auto wgs = [&](int64_t per) {
       int64_t w = 0;
@@ -469,7 +475,6 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
     };
     // row tiles of a wave: rounds of the workgroups that run at once (three of four waves or one of eight a
     // CU) times a workgroup's time, its start as long as 90 KB of a CU's weights; tiles as even groups give
-    const int64_t used = c.er.count < c.er.n ? c.er.count : c.er.n, tiles_even = used * ceil_div(c.er.n / used, 16 * ct);
     const int64_t at_once = 256 * (ct == 1 ? 3 : 1);
     const int64_t step = (ct == 1 ? 192 : 128) * c.K * 23 / 32;  // a CU's bytes for one row tile a wave, a quarter dense
     int64_t best = 0;
@@ -488,7 +493,8 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
   const hipError_t e = stream_kernel ? (ct == 1   ? spense::launch_stream<1, 4>(a, c.er, grid, (int)lds, stream)
                                         : ct == 2 ? spense::launch_stream<2, 8>(a, c.er, grid, (int)lds, stream)
                                                   : spense::launch_stream<4, 8>(a, c.er, grid, (int)lds, stream))
-                                     : (ct == 1   ? spense::launch_rows<1, 4>(a, c.er, grid, stream)
+                                     : (wv == 2   ? spense::launch_rows<1, 2>(a, c.er, grid, stream)
+                                        : wv == 4 ? spense::launch_rows<1, 4>(a, c.er, grid, stream)
                                                   : spense::launch_rows<2, 8>(a, c.er, grid, stream));
   return e == hipSuccess ? SPENSE_OK : api_fail(SPENSE_ERR_HIP, "experts launch failed: %s", hipGetErrorString(e));
 }

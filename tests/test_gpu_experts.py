@@ -97,6 +97,23 @@ def test_experts_exact(S, T, top, E, N, K, split, db, kind):
         assert torch.all(y[n:] == 9)  # rows of no expert
 
 
+LONG = [  # K beyond what the short-K kernel keeps in LDS: two and four waves a workgroup, tiles of 16 and 32
+    (1, 2, 3, 208, 3616, 0, 160), (3, 2, 5, 130, 3744, 1, 1600), (8, 1, 8, 1601, 3616, 0, 1200), (20, 2, 2, 257, 4096, 0, 128),
+    (37, 2, 4, 96, 4128, 1, 4096), (9, 3, 3, 48, 5120, 1, 0),
+]
+
+
+@pytest.mark.parametrize("T,top,E,N,K,split,db", LONG)
+@pytest.mark.parametrize("kind", ["even", "one"])
+def test_long_rows_exact(S, T, top, E, N, K, split, db, kind):
+    test_experts_exact(S, T, top, E, N, K, split, db, kind)
+
+
+@pytest.mark.parametrize("T,top,E,N,K,split,db", LONG)
+def test_long_rows_random(S, T, top, E, N, K, split, db):
+    test_experts_random(S, T, top, E, N, K, split, db)
+
+
 LARGE = [  # many rows an expert: tiles of up to 128 positions, and (from 256 of those on) of 256
     (450, 1, 2, 300, 352, 0, 112), (520, 2, 2, 136, 256, 0, 136), (640, 1, 1, 400, 1056, 1, 1056), (999, 3, 5, 264, 480, 1, 0),
     (1040, 1, 8, 2200, 288, 0, 1648), (700, 2, 9, 2065, 352, 1, 160), (530, 2, 11, 2190, 256, 0, 0), (1300, 1, 6, 3200, 320, 1, 320),
