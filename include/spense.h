@@ -641,7 +641,7 @@ size_t spense_adapters_workspace_size(int64_t M, const spense_adapters_t* pool);
  * SPENSE_ERR_ARG for NULL pointers, bad sizes (M above SPENSE_MAX_GROUP_ROWS, M x N too large for a
  * launch) or types, an R or count outside the limits above,
  * ld below the row length, a Y = base of another type or pitch, X or one adapter of 2 GiB or
- * more; SPENSE_ERR_ALIGN for X, A, B or ws not 16-byte aligned (ldx a multiple of 16 bytes),
+ * more; SPENSE_ERR_ALIGN for X, A, B or ws not 16-byte aligned (ldx a multiple of 16 bytes where M > 1),
  * K % 32, base or Y not aligned to its elements; SPENSE_ERR_WS for a missing or small workspace.
  */
 int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, const float* x_scale, const int32_t* order,
@@ -668,7 +668,7 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
  * Asynchronous, allocates nothing.  SPENSE_ERR_ARG for NULL pointers, weights outside [1, 2],
  * count outside [1, SPENSE_MAX_GROUPS], top below 1, bad sizes (n above SPENSE_MAX_GROUP_ROWS, n x N
  * too large for a launch) or flags, Y[1] = Y[0], mixed or unsupported weights, K = 0, ld below the row length, an X or one expert's buffer of 2 GiB or more;
- * SPENSE_ERR_ALIGN for a misaligned X, Y or weight.
+ * SPENSE_ERR_ALIGN for a misaligned X (16 bytes, with rows_x > 1 ldx a multiple of 16), Y or weight.
  */
 int spense_gemm_experts(const void* X, int64_t rows_x, int64_t ldx, const float* x_scale, const int32_t* order, int32_t top,
                         const int32_t* offsets, int64_t n, int32_t count, int32_t weights,

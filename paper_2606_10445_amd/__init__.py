@@ -1133,6 +1133,8 @@ def gemm_adapters(X: torch.Tensor, pw: PackedWeight, pool: AdapterPool, groups: 
     unquantised output of block_norm)."""
     if pw.N != pool.N:
         raise ValueError(f"the weight has {pw.N} rows, the adapters {pool.N}")
+    if X.dim() == 2 and X.shape[0] == 1 and X.stride(1) == 1:
+        X = X.as_strided(X.shape, (X.shape[1], 1))  # a single row's stride does not matter
     base = gemm(X, pw, w_scale, x_scale, out_f32=True, workspace=workspace)
     if A_x is not None:
         X, x_scale = A_x, None

@@ -458,7 +458,8 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   const int64_t xs = x_type == SPENSE_BF16 ? 2 : 1, bs = base_type == SPENSE_BF16 ? 2 : 4,
                 ys = (out_flags & SPENSE_OUT_F32) ? 4 : 2;
   auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
-  if (at(X) % 16 || (ldx * xs) % 16) return api_fail(SPENSE_ERR_ALIGN, "X must be 16-byte aligned with a 16-byte multiple row pitch");
+  if (at(X) % 16 || (M > 1 && (ldx * xs) % 16))
+    return api_fail(SPENSE_ERR_ALIGN, "X must be 16-byte aligned with a 16-byte multiple row pitch");
   if (at(P.A) % 16 || at(P.B) % 16) return api_fail(SPENSE_ERR_ALIGN, "A and B must be 16-byte aligned");
   if (at(base) % bs || at(Y) % ys) return api_fail(SPENSE_ERR_ALIGN, "base or Y misaligned");
   const bool same = base == Y;

@@ -375,7 +375,7 @@ int check_call(Call& c, const void* X, int64_t rows_x, int64_t ldx, const float*
   if (c.K < 1) return api_fail(SPENSE_ERR_ARG, "K=0");
   if (!X || !offsets) return api_fail(SPENSE_ERR_ARG, "X or offsets is NULL");
   if (ldx < c.K) return api_fail(SPENSE_ERR_ARG, "ldx=%lld < K=%lld", (long long)ldx, (long long)c.K);
-  if (reinterpret_cast<uintptr_t>(X) % 16 || ldx % 16)
+  if (reinterpret_cast<uintptr_t>(X) % 16 || (rows_x > 1 && ldx % 16))
     return api_fail(SPENSE_ERR_ALIGN, "X must be 16-byte aligned with a 16-byte multiple row pitch");
   const int64_t lim = (int64_t)1 << 31;
   c.X = static_cast<const uint8_t*>(X), c.ldx = ldx, c.xb = rows_x > 0 ? (rows_x - 1) * ldx + c.K : 0, c.x_scale = x_scale;

@@ -239,6 +239,29 @@ def test_gemm_adapters(S, M):
         assert torch.equal(y, S.add_adapters(base, x, pool, g, out_f32=f32))
 
 
+@pytest.mark.parametrize("x", ["fp8", "bf16"])
+def test_one_row_of_an_odd_pitch(S, x):
+    """A single token that is a row of a wider buffer, whatever the pitch (one row has none), in
+    add_adapters and in gemm_adapters."""
+    import gen
+
+    N, K, R, count = 512, 1024, 16, 5
+    t = inputs(17, 1, K, N, R, count, x, "f32", idx=torch.tensor([3]))
+    pool, g, bd = S.AdapterPool(*(v.cuda() for v in t[2:5])), S.group_rows(t[6].cuda(), count), t[5].cuda()
+    X, xs = t[0].cuda(), None if t[1] is None else t[1].cuda()
+    X = X.view(torch.uint8) if x == "fp8" else X
+    ref = S.add_adapters(bd, X, pool, g, x_scale=xs)
+    wide = torch.zeros(3, K + 5, dtype=X.dtype, device="cuda")
+    wide[0, :K] = X[0]
+    for row in (wide[:1, :K], wide[0, :K].expand(1, K)):
+        assert torch.equal(S.add_adapters(bd, row, pool, g, x_scale=xs), ref)
+    if x == "fp8":
+        mx = gen.make_matrix(3, 0, "w", N, K, gen.OUTPUT, 0.25, gen.FP8)
+        pw = S.tile(S.compress(torch.from_numpy(mx.W).cuda(), torch.from_numpy(mx.mask).cuda(), 0, mx.dense_begin))
+        sw = torch.from_numpy(mx.sw).cuda()
+        assert torch.equal(S.gemm_adapters(wide[:1, :K], pw, pool, g, sw, xs), S.gemm_adapters(X, pw, pool, g, sw, xs))
+
+
 def test_binding_refuses(S):
     t = inputs(1, 8, 64, 32, 8, 2, "bf16", "f32")
     X, _, A, B, sc, bd, idx = [None if v is None else v.cuda() for v in t]

@@ -178,3 +178,22 @@ def test_glu_workspace_size(S):
         for count in (1, 5, 64, 1024):
             for N in (1, 16, 100, 1536, 25600):
                 assert n * N * 4 < size(n, count, N) <= 2 * (n * (N + 63) * 4 + 256)
+
+
+def test_the_pitch_of_a_single_row_does_not_matter(S):
+    """One activation row may come from a buffer of any pitch; seen by the next refusal of such a call."""
+    import ctypes
+
+    args = dict(X=A, x_type=2, M=1, ldx=65, x_scale=None, order=A, offsets=A, pool=pool(S), base=A, base_type=3, ldb=48,
+                Y=2 * A, ldy=48, out_flags=0, ws=None, ws_bytes=0, stream=None)
+    assert S.spense_add_adapters(**args) == -4
+    assert S.spense_add_adapters(**{**args, "x_type": 1}) == -4
+    assert S.spense_add_adapters(**{**args, "M": 2}) == -2
+    assert S.spense_add_adapters(**{**args, "ldx": 63}) == -1
+    d = S.spense_packed_t(1, 0, 64, 128, 32, A, 64, A, 4, A, 128, 1)
+
+    def glu(rows_x, ldx):
+        return S.spense_gemm_experts_glu_fp8(A, rows_x, ldx, None, A, 8, A, 8, 4, ctypes.byref(d), ctypes.byref(d), None,
+                                             None, A, 64, A, None, 0, None)
+
+    assert glu(1, 129) == -4 and glu(2, 129) == -2 and glu(1, 127) == -1
