@@ -1135,7 +1135,9 @@ def gemm_adapters(X: torch.Tensor, pw: PackedWeight, pool: AdapterPool, groups: 
         raise ValueError(f"the weight has {pw.N} rows, the adapters {pool.N}")
     if X.dim() == 2 and X.shape[0] == 1 and X.stride(1) == 1:
         X = X.as_strided(X.shape, (X.shape[1], 1))  # a single row's stride does not matter
-    base = gemm(X, pw, w_scale, x_scale, out_f32=True, workspace=workspace)
+    _on_gpu(X.device, A_x, pw.dense, pool.A)
+    with _device(X.device):
+        base = gemm(X, pw, w_scale, x_scale, out_f32=True, workspace=workspace)
     if A_x is not None:
         X, x_scale = A_x, None
     return add_adapters(base, X, pool, groups, x_scale, out=base if out_f32 and out is None else out, out_f32=out_f32,

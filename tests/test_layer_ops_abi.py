@@ -197,3 +197,37 @@ def test_the_pitch_of_a_single_row_does_not_matter(S):
                                              None, A, 64, A, None, 0, None)
 
     assert glu(1, 129) == -4 and glu(2, 129) == -2 and glu(1, 127) == -1
+
+
+def test_gemm_adapters_makes_its_device_current(S, monkeypatch):
+    """The projection of gemm_adapters runs with the tensors' device current, as the adapters do."""
+    import contextlib
+    from types import SimpleNamespace
+
+    import torch
+
+    entered, calls = [], []
+
+    @contextlib.contextmanager
+    def device(dev):
+        entered.append(dev)
+        yield
+        entered.pop()
+
+    monkeypatch.setattr(S, "_device", device)
+    monkeypatch.setattr(S, "_on_gpu", lambda dev, *tensors: None)
+    monkeypatch.setattr(S, "gemm", lambda X, *a, **kw: calls.append(list(entered)) or X)
+    monkeypatch.setattr(S, "add_adapters", lambda base, *a, **kw: base)
+    X = torch.zeros(2, 32)
+    S.gemm_adapters(X, SimpleNamespace(N=8, dense=X), SimpleNamespace(N=8, A=X), None)
+    assert calls == [[X.device]]
+
+
+def test_gemm_adapters_refuses_tensors_on_the_cpu(S):
+    from types import SimpleNamespace
+
+    import torch
+
+    X = torch.zeros(2, 32)
+    with pytest.raises(ValueError, match="GPU"):
+        S.gemm_adapters(X, SimpleNamespace(N=8, dense=X), SimpleNamespace(N=8, A=X), None)
