@@ -542,7 +542,7 @@ int spense_obs_prune_24(float* W, int64_t ldw, int64_t N, int64_t K, const float
  * Asynchronous, allocates nothing.
  * SPENSE_ERR_ARG for a NULL x, no output, q without scales, a gate or post_weight without y,
  * M below 0 or too large, K below 1 or above 2^31-1, residual in the place of y or normed, normed in the
- * place of x, ld below K, unknown types, a negative or non-finite eps;
+ * place of x, an output in its input's place with another leading dimension (M > 1), ld below K, unknown types, a negative or non-finite eps;
  * SPENSE_ERR_ALIGN for an operand not aligned to its elements.
  */
 typedef struct spense_block_norm_t {

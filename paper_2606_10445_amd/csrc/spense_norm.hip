@@ -416,6 +416,9 @@ extern "C" int spense_block_norm(const spense_block_norm_t* p, hipStream_t strea
   if (b.residual && (b.residual == b.y || b.residual == b.normed))
     return api_fail(SPENSE_ERR_ARG, "the residual in the place of y or of normed");
   if (b.normed && b.normed == b.x) return api_fail(SPENSE_ERR_ARG, "normed in the place of x");
+  // in place, each thread overwrites what it alone has read: with another pitch it would be another row's
+  if (b.M > 1 && ((b.residual && b.residual == b.x && b.ldr != b.ldx) || (b.normed && b.normed == b.y && b.ldn != b.ldy)))
+    return api_fail(SPENSE_ERR_ARG, "an output in the place of its input must have its leading dimension");
   if (!spense::grid_fits(b.M + 255, spense::row_lanes(b.K))) return api_fail(SPENSE_ERR_ARG, "M=%lld too large for the grid", (long long)b.M);
   const int64_t xs = b.x_type == SPENSE_BF16 ? 2 : 4, ys = b.y_type == SPENSE_BF16 ? 2 : 4,
                 ws = b.w_type == SPENSE_BF16 ? 2 : 4;

@@ -33,6 +33,16 @@ def test_block_norm_refuses(S, kw, code):
     assert S.spense_last_error()
 
 
+@pytest.mark.parametrize("kw", [dict(residual=A, ldr=72), dict(normed=A, ldn=72), dict(residual=A, ldx=72),
+                                dict(normed=A, ldy=128, K=32)])
+def test_block_norm_refuses_an_input_overwritten_at_another_pitch(S, kw):
+    """In place, a row's outputs would go over other rows' inputs before these are read."""
+    x, y = (A, 5 * A) if "residual" in kw else (5 * A, A)
+    base = dict(x=x, y=y, residual=6 * A, normed=7 * A, q=8 * A, gate=9 * A, weight=10 * A, post_weight=11 * A)
+    assert S.spense_block_norm(norm_args(S, **{**base, **kw}), None) == -1
+    assert "leading dimension" in S.spense_last_error()
+
+
 def test_block_norm_of_nothing(S):
     assert S._lib.spense_block_norm(None, None) == -1
     assert S.spense_block_norm(norm_args(S, K=0), None) == -1
