@@ -708,7 +708,7 @@ int spense_abi_version(void);
  * >= 1 every call that makes a new plan for a single weight (the planner's choice for one
  * dtype, M and weight geometry; later calls with the same key reuse it) writes one line to
  * stderr naming the kernel and its shape; with level >= 2 every grouped and paired call
- * does too.  The level starts at the value of the environment variable SPENSE_LOG when
+ * does too, those over rows grouped by expert and spense_add_adapters among them.  The level starts at the value of the environment variable SPENSE_LOG when
  * the library is loaded (0 when unset or not a number); it is read there only.  The log
  * never changes a plan or a result.  Returns the previous level; thread-safe.
  */

@@ -14,6 +14,8 @@
 //
 // Memory-bound: for prompts by base and Y (6 bytes an output against 2 R multiply-adds), for
 // decoding by A and B of the adapters in the batch.
+#include <cstdio>
+
 #include "spense_gemm_device.h"
 #include "spense_rows_device.h"
 
@@ -480,6 +482,9 @@ int spense_add_adapters(const void* X, int32_t x_type, int64_t M, int64_t ldx, c
   const int64_t nblocks = (P.N + 128 * steps - 1) / (128 * steps);
   if (!spense::grid_fits(all_tiles * nblocks, 256)) return api_fail(SPENSE_ERR_ARG, "M x N too large for the grid");
   const size_t need = spense_adapters_workspace_size(M, pool);
+  if (spense::api_log_level() >= 2)
+    fprintf(stderr, "spense: adapters M=%lld count=%d R=%d K=%lld N=%lld -> tile_tokens=%d k_slices=%d steps=%d workspace=%zu\n",
+            (long long)M, P.count, P.R, (long long)P.K, (long long)P.N, T, spense::k_slices(M, P.count, P.K, P.R), steps, need);
   if (!ws || ws_bytes < need) return api_fail(SPENSE_ERR_WS, "workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
   if (at(ws) % 16) return api_fail(SPENSE_ERR_ALIGN, "workspace must be 16-byte aligned");
   int rc = spense::api_check_device();

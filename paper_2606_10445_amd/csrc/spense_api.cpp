@@ -1216,6 +1216,8 @@ int api_ok() { return ok(); }
 
 int api_check_device() { return check_device(); }
 
+int api_log_level() { return g_log.load(std::memory_order_relaxed); }
+
 int api_check_packed(const spense_packed_t* P) {
   spense_layout_t L;
   return check_packed(P, &L);

@@ -11,6 +11,7 @@
 // short K, in tiles of up to 64 positions.
 // Many rows: the 128 x 128 and 256 x 256 kernels over tiles of positions (spense_gemm_mid.hip,
 // spense_gemm_big2.hip).
+#include <cstdio>
 #include <cstring>
 
 #include "spense_gemm_device.h"
@@ -411,6 +412,16 @@ void set_output(Call& c, int i, void* Y, int64_t ldy, bool f32) {
   c.mat[i].vec_store = 1;  // at any alignment of the elements
 }
 
+// The dispatch log's line of a launch: positions of a tile, waves of a workgroup, row tiles of a wave, row blocks.
+void log_launch(const Call& c, const char* kernel, int positions, int waves, int tiles_wave, int64_t blocks) {
+  if (spense::api_log_level() < 2) return;
+  fprintf(stderr,
+          "spense: experts n=%d count=%d weights=%d N=%lld K=%lld split=%s dense_begin=%lld -> %s positions=%d waves=%d "
+          "tiles_wave=%d row_blocks=%lld\n",
+          c.er.n, c.er.count, c.weights, (long long)c.N, (long long)c.K, c.in_split ? "input" : "output", (long long)c.db, kernel,
+          positions, waves, tiles_wave, (long long)blocks);
+}
+
 // A launch of the 128 x 128 or, with `big`, the 256 x 256 kernel; pmax: the gate / up pair, the
 // fp32 H to mat[0].Y and its row maxima (pmax_ld of them a row) to pmax.
 int launch_tiles(Call& c, bool big, float* pmax, int64_t pmax_ld, hipStream_t stream) {
@@ -435,6 +446,7 @@ int launch_tiles(Call& c, bool big, float* pmax, int64_t pmax_ld, hipStream_t st
   g.groups = (int32_t)blocks, g.hg0 = g.groups;
   if (!spense::grid_fits(spense::most_tiles(c.er.n, c.er.count, false, big ? 256 : 128) * blocks + 8, big ? 512 : 768))
     return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
+  log_launch(c, !big ? "128x128" : pmax ? "256x256, gate/up paired" : "256x256", big ? 256 : 128, big ? 8 : 12, 1, blocks);
   int rc = spense::api_check_device();
   if (rc) return rc;
   const hipError_t e = big ? spense::launch_experts_big2(g, c.er, stream) : spense::launch_experts_mid(g, c.er, stream);
@@ -488,6 +500,7 @@ int launch_few(Call& c, int64_t chunks, int ct, hipStream_t stream) {
   }
   const int64_t grid = most * a.wgs;
   if (!spense::grid_fits(grid, 64 * wv)) return api_fail(SPENSE_ERR_ARG, "n x N too large for the grid");
+  log_launch(c, stream_kernel ? "stream" : "rows", 16 * ct, wv, stream_kernel ? a.tiles_wave : 1, a.wgs);
   int rc = spense::api_check_device();
   if (rc) return rc;
   const hipError_t e = stream_kernel ? (ct == 1   ? spense::launch_stream<1, 4>(a, c.er, grid, (int)lds, stream)

@@ -143,6 +143,8 @@ int api_fail(int code, const char* fmt, ...);
 int api_ok();
 int api_check_device();
 int api_check_packed(const spense_packed_t* P);
+// The level of the dispatch log (spense_set_log).
+int api_log_level();
 
 // Whether a launch of this many workgroups fits the runtime's 32-bit count of work items.
 inline bool grid_fits(int64_t workgroups, int64_t threads) { return workgroups <= UINT32_MAX / threads; }

@@ -5,6 +5,7 @@ compared bit for bit.  Random cases: the fp8 matrix instructions add the product
 chunk with 13 fractional bits of the largest, so a sum is within (2^-12 + 2 K u) of the sum of
 magnitudes (u = 2^-24), then two scales and half a step of the output type.
 """
+import re
 import sys
 
 import pytest
@@ -422,3 +423,77 @@ def test_binding_refuses(S):
     with pytest.raises(ValueError):
         S.mlp_experts(X, torch.ones(6, device="cuda"), torch.zeros(5, 2, dtype=torch.int32, device="cuda"),
                       torch.zeros(5, 2, device="cuda"), pe, pe, pe)
+
+
+# Sizes at which the short-K kernel gives a wave several row tiles (the rule goes by the sizes only; what it chooses is
+# in the dispatch log and checked): rows of activations, experts, N, K, split, dense_begin, weights -> positions
+# of a tile, row tiles of a wave.  Their last workgroups give waves fewer tiles than that, or none.
+STREAMS = [
+    (135, 27, 1746, 160, 0, 1296, 1, 16, 2), (264, 44, 1046, 1056, 0, 720, 1, 16, 2), (165, 55, 1677, 160, 1, 96, 1, 16, 3),
+    (53, 53, 1803, 1056, 1, 736, 1, 16, 3), (330, 55, 2404, 160, 0, 2400, 1, 16, 4), (385, 55, 2526, 1056, 1, 768, 1, 16, 4),
+    (60, 60, 3077, 160, 1, 64, 1, 16, 5), (260, 52, 4185, 160, 0, 4176, 1, 16, 6), (224, 56, 4837, 160, 0, 4832, 1, 16, 7),
+    (480, 60, 4963, 704, 0, 4960, 1, 16, 8), (39, 39, 1066, 160, 0, 528, 2, 16, 3), (110, 55, 2424, 160, 0, 1808, 2, 16, 8),
+    (896, 56, 445, 160, 0, 304, 1, 32, 2), (742, 53, 445, 1056, 0, 304, 1, 32, 2), (520, 52, 1050, 160, 1, 0, 1, 32, 3),
+    (986, 58, 1028, 1056, 1, 768, 1, 32, 3), (731, 43, 1976, 160, 1, 96, 1, 32, 4), (792, 44, 1558, 1056, 0, 1168, 1, 32, 4),
+    (520, 52, 1662, 160, 0, 1648, 1, 32, 5), (688, 43, 3242, 160, 1, 64, 1, 32, 6), (880, 55, 2385, 160, 0, 2384, 1, 32, 7),
+    (583, 53, 2888, 160, 0, 2880, 1, 32, 8), (731, 43, 368, 160, 0, 272, 2, 32, 3), (688, 43, 1220, 160, 0, 912, 2, 32, 8),
+    (2585, 55, 485, 160, 0, 352, 1, 64, 2), (1456, 52, 422, 1120, 0, 288, 1, 64, 2), (1040, 52, 1029, 160, 1, 64, 1, 64, 3),
+    (1357, 59, 1036, 1056, 1, 736, 1, 64, 3), (1720, 43, 1303, 1056, 0, 912, 1, 64, 3), (1664, 52, 1320, 160, 0, 912, 1, 64, 4),
+    (2120, 53, 2081, 160, 1, 96, 1, 64, 5), (1196, 52, 1995, 160, 0, 1984, 1, 64, 6), (1908, 53, 3100, 160, 1, 0, 1, 64, 7),
+    (900, 40, 5120, 1408, 1, 1056, 1, 64, 7), (1484, 53, 2841, 160, 0, 2832, 1, 64, 8), (1204, 43, 405, 160, 0, 288, 2, 64, 3),
+    (1333, 43, 1225, 160, 0, 912, 2, 64, 8),
+]
+
+
+def launches(capfd):
+    """(kernel, positions of a tile, row tiles of a wave) of the grouped products in the dispatch log."""
+    line = re.compile(r"spense: experts .* -> (.*) positions=(\d+) waves=\d+ tiles_wave=(\d+) ")
+    return [(m[1], int(m[2]), int(m[3])) for m in map(line.match, capfd.readouterr().err.splitlines()) if m]
+
+
+def weights_on_gpu(S, g, E, N, K, split, db):
+    """As ``weights`` with integers, drawn on the GPU: (PackedExperts, E x N x K values (float8), E x N scales)."""
+    q = torch.empty(E, N, K, dtype=torch.float8_e4m3fn, device="cuda")
+    pws = []
+    for e in range(E):
+        w = torch.randint(-3, 4, (N, K), generator=g, device="cuda").float()
+        reg = w[:db] if split == 0 else w[:, :db]
+        if reg.numel():
+            r = torch.rand(reg.shape[0], reg.shape[1] // 4, 4, generator=g, device="cuda")
+            keep = torch.zeros_like(r).scatter_(-1, r.argsort(-1)[..., :2], 1.0)
+            reg.copy_((reg.reshape(r.shape) * keep).reshape(reg.shape))
+        q[e] = w.to(torch.float8_e4m3fn)
+        pws.append(S.tile(S.compress(q[e].view(torch.uint8), (w != 0).to(torch.uint8), split, db)))
+    return S.stack_experts(pws), q, 2.0 ** torch.randint(-2, 3, (E, N), generator=g, device="cuda").float()
+
+
+@pytest.mark.parametrize("n,E,N,K,split,db,k,positions,tiles", STREAMS)
+def test_several_row_tiles_a_wave(S, capfd, n, E, N, K, split, db, k, positions, tiles):
+    """A wave's second row tile and those after it: addresses, scales, sums begun anew, the ragged last workgroup."""
+    say(f"[experts] n={n} E={E} {N}x{K} split={split} db={db} weights={k}")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + N + K)
+    ws = [weights_on_gpu(S, g, E, N, K, split, db) for _ in range(k)]
+    x = torch.randint(-3, 4, (n, K), generator=g, device="cuda").to(torch.float8_e4m3fn)
+    xs = 2.0 ** torch.randint(-2, 3, (n,), generator=g, device="cuda").float()
+    idx = (torch.rand(n, generator=g, device="cuda") ** 1.5 * (E + 1)).int() - 1  # uneven; some in no group
+    idx[idx == E // 2] = 0  # an expert without rows
+    groups = S.group_rows(idx, E)
+    order, offsets = groups.order.long(), groups.offsets.tolist()
+    for f32 in (False, True):
+        dt = torch.float32 if f32 else torch.bfloat16
+        outs = [torch.full((n, N), 9.0, dtype=dt, device="cuda") for _ in range(k)]
+        prev = S.spense_set_log(2)
+        try:
+            capfd.readouterr()
+            S.gemm_experts(x.view(torch.uint8), [w[0] for w in ws], groups, [w[2] for w in ws], xs, outs=outs, out_f32=f32)
+            assert launches(capfd) == [("stream", positions, tiles)]
+        finally:
+            S.spense_set_log(prev)
+        for y, (_, q, sc) in zip(outs, ws):
+            for e in range(E):
+                a, b = offsets[e], offsets[e + 1]
+                acc = x[order[a:b]].double() @ q[e].double().t().contiguous()
+                want = acc * sc[e].double() * xs[order[a:b], None].double()
+                assert torch.equal(y[a:b], want.float().to(dt)), f"expert {e}"
+            assert torch.all(y[offsets[E]:] == 9)

@@ -241,3 +241,26 @@ def test_gemm_adapters_refuses_tensors_on_the_cpu(S):
     X = torch.zeros(2, 32)
     with pytest.raises(ValueError, match="GPU"):
         S.gemm_adapters(X, SimpleNamespace(N=8, dense=X), SimpleNamespace(N=8, A=X), None)
+
+
+def test_row_tiles_a_wave_rule(S, capfd):
+    """The short-K kernel and its row tiles a wave at the sizes that the GPU tests of them take, by the dispatch log."""
+    import ctypes
+
+    import torch
+    from test_gpu_experts import STREAMS, launches
+
+    if torch.cuda.is_available():
+        pytest.skip("made-up addresses: the calls must end at the device check")
+    prev = S.spense_set_log(2)
+    try:
+        for n, E, N, K, split, db, k, positions, tiles in STREAMS:
+            d = S.spense_packed_t(1, split, N, K, db, A, K, A, K, A, K, 1)
+            parr = (ctypes.POINTER(S.spense_packed_t) * k)(*[ctypes.pointer(d)] * k)
+            yarr, larr = (ctypes.c_void_p * k)(*[A * (2 + i) for i in range(k)]), (ctypes.c_int64 * k)(*[N] * k)
+            capfd.readouterr()
+            assert S.spense_gemm_experts(A, n, K, None, A, 1, A, n, E, k, parr, None, yarr, larr, 0, None) < 0
+            assert launches(capfd) == [("stream", positions, tiles)]
+    finally:
+        S.spense_set_log(prev)
+    assert {(t[7], t[8]) for t in STREAMS} == {(p, t) for p in (16, 32, 64) for t in range(2, 9)}
