@@ -4,6 +4,7 @@ A x is a sum of K fp32 products (at most K + 40 roundings of u = 2^-24 with the 
 the two scales), V = s A x enters B V within 2^-17, B V is a sum of 2 R products, base and the
 rounding of Y follow.  On small integers every one of these is exact.
 """
+import re
 import sys
 
 import pytest
@@ -99,6 +100,46 @@ def test_integers_exact(S, M, K, N, R, count, x):
     say(f"[adapters exact] M={M} K={K} N={N} R={R} count={count} {x}")
     y = call(S, t, count, out_f32=True).cpu().double()
     assert torch.equal(y, formula(*t)[0])
+
+
+# Sizes at which a workgroup of the second launch takes more than two steps of 128 columns (by a rule on the sizes;
+# what it chooses is in the dispatch log and checked): M, K, N, R, count -> tokens of a tile, steps.  N ends in
+# different steps, inside a piece of eight and of 32 columns and between them.
+WIDE = [
+    (64, 64, 8201, 16, 64, 16, 8), (64, 32, 25601, 8, 64, 16, 8), (96, 64, 6657, 64, 90, 16, 8), (160, 64, 7004, 128, 150, 16, 8),
+    (64, 64, 5003, 24, 64, 16, 4), (100, 96, 3360, 40, 90, 16, 4), (64, 544, 4097, 16, 64, 16, 4), (2048, 64, 8190, 64, 16, 32, 4),
+    (2048, 64, 4001, 16, 16, 32, 4), (1024, 96, 8328, 32, 8, 32, 4), (520, 64, 16385, 8, 5, 32, 4),
+]
+
+
+def chosen(capfd):
+    """(tokens of a tile, steps) of the adapter calls in the dispatch log."""
+    line = re.compile(r"spense: adapters .* -> tile_tokens=(\d+) k_slices=\d+ steps=(\d+) ")
+    return [(int(m[1]), int(m[2])) for m in map(line.match, capfd.readouterr().err.splitlines()) if m]
+
+
+@pytest.mark.parametrize("M,K,N,R,count,tokens,steps", WIDE)
+@pytest.mark.parametrize("base", ["f32", "bf16"])
+def test_many_columns_a_workgroup(S, capfd, M, K, N, R, count, tokens, steps, base):
+    """Exact integers with fp32 outputs, random values with the base's type, and the latter over base itself."""
+    say(f"[adapters wide] M={M} K={K} N={N} R={R} count={count} {base}")
+    prev = S.spense_set_log(2)
+    try:
+        t = inputs(M + N, M, K, N, R, count, "fp8", base, ints=True)
+        capfd.readouterr()
+        assert torch.equal(call(S, t, count, out_f32=True).cpu().double(), formula(*t)[0])
+        assert chosen(capfd) == [(tokens, steps)]
+    finally:
+        S.spense_set_log(prev)
+    t = inputs(M + N, M, K, N, R, count, "bf16", base)
+    y = call(S, t, count, out_f32=base == "f32")
+    want, e = formula(*t)
+    assert torch.all((y.cpu().double() - want).abs() <= e + (U if base == "f32" else 2.0 ** -8) * (want.abs() + e) + 1e-38)
+    pool, g = S.AdapterPool(*(v.cuda() for v in t[2:5])), S.group_rows(t[6].cuda(), count)
+    over = torch.full((M, N + 3), 5.0, dtype=t[5].dtype, device="cuda")
+    over[:, :N] = t[5].cuda()
+    S.add_adapters(over[:, :N], t[0].cuda(), pool, g, out=over[:, :N], out_f32=base == "f32")
+    assert torch.equal(over[:, :N], y) and torch.all(over[:, N:] == 5)
 
 
 @pytest.mark.parametrize("kind", ["none", "one", "runs", "last"])

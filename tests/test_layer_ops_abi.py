@@ -264,3 +264,20 @@ def test_row_tiles_a_wave_rule(S, capfd):
     finally:
         S.spense_set_log(prev)
     assert {(t[7], t[8]) for t in STREAMS} == {(p, t) for p in (16, 32, 64) for t in range(2, 9)}
+
+
+def test_adapter_columns_rule(S, capfd):
+    """Tokens of a tile and steps of a workgroup at the sizes that the GPU tests of them take, by the dispatch log;
+    the calls end at the missing workspace."""
+    from test_gpu_adapters import WIDE, chosen
+
+    prev = S.spense_set_log(2)
+    try:
+        for M, K, N, R, count, tokens, steps in WIDE:
+            capfd.readouterr()
+            assert S.spense_add_adapters(A, 2, M, K, None, A, A, pool(S, count=count, R=R, K=K, N=N), A, 3, N, 2 * A, N, 0,
+                                         None, 0, None) == -4
+            assert chosen(capfd) == [(tokens, steps)]
+    finally:
+        S.spense_set_log(prev)
+    assert {t[5:] for t in WIDE} == {(16, 4), (16, 8), (32, 4)}
