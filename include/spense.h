@@ -638,6 +638,9 @@ size_t spense_adapters_workspace_size(int64_t M, const spense_adapters_t* pool);
  * rounded once.  The order of the sums depends on the sizes only.  Two launches, asynchronous;
  * ws is scratch between them, caller-owned; calls that overlap on one workspace race.
  * order entries outside [0, M) are skipped, offsets are clamped to [0, M].
+ * Tokens that are not finite, and entries of A and B, reach the rows and columns that the formula takes them
+ * to; but an infinite entry of B gives NaN there, also where the formula is infinite (V enters the product
+ * as the sum of two numbers), and a V above bfloat16's range counts as infinite.
  * SPENSE_ERR_ARG for NULL pointers, bad sizes (M above SPENSE_MAX_GROUP_ROWS, M x N too large for a
  * launch) or types, an R or count outside the limits above,
  * ld below the row length, a Y = base of another type or pitch, X or one adapter of 2 GiB or

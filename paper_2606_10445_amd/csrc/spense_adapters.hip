@@ -10,7 +10,8 @@
 // Roundings: fp8 codes and bf16 activations enter the matrix instructions exactly (every
 // e4m3fn value is a bf16 value), sums are fp32.  V enters the second product as two bf16
 // numbers, hi + lo, 2^-17 of V off at most; the matrix work that doubles is far from the
-// bound.  Y is rounded once.
+// bound.  (An infinite entry of B times lo, which may be zero or of the other sign, makes NaN of an
+// infinite sum.)  Y is rounded once.
 //
 // Memory-bound: for prompts by base and Y (6 bytes an output against 2 R multiply-adds), for
 // decoding by A and B of the adapters in the batch.

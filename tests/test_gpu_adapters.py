@@ -213,6 +213,19 @@ def test_non_finite_tokens_stay_alone(S):
     assert torch.all(torch.isnan(y[5])) and torch.all(torch.isfinite(y[6]))
 
 
+def test_non_finite_entries_of_a_pool_stay_where_they_belong(S):
+    """An infinity or NaN in A reaches its adapter's tokens, one in B one column of these; nothing else changes."""
+    M, K, N, R, count = 40, 256, 72, 16, 3
+    t = inputs(4, M, K, N, R, count, "bf16", "f32", idx=torch.arange(M) % (count + 1))
+    clean = call(S, t, count, out_f32=True)
+    t[2][0, 5, 7], t[3][1, 33, 2], t[3][2, 70, 11] = float("inf"), float("inf"), float("nan")
+    y = call(S, t, count, out_f32=True)
+    hit = torch.zeros(M, N, dtype=torch.bool)
+    hit[t[6] == 0], hit[t[6] == 1, 33], hit[t[6] == 2, 70] = True, True, True
+    hit = hit.cuda()
+    assert torch.equal(y[~hit], clean[~hit]) and not torch.any(torch.isfinite(y[hit]))
+
+
 def test_rows_outside_are_skipped(S):
     """order and offsets of another making: entries outside [0, M) and offsets past M name nothing."""
     M, K, N, R = 40, 64, 128, 8
