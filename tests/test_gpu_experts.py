@@ -497,3 +497,101 @@ def test_several_row_tiles_a_wave(S, capfd, n, E, N, K, split, db, k, positions,
                 want = acc * sc[e].double() * xs[order[a:b], None].double()
                 assert torch.equal(y[a:b], want.float().to(dt)), f"expert {e}"
             assert torch.all(y[offsets[E]:] == 9)
+
+
+def glu_bounds(x, xs, W, sc, src):
+    """(value, bound) in 64 bits of rows src times one expert's weight: the error of ``check`` before rounding."""
+    f = sc.double()[None, :] * xs[src].double()[:, None]
+    acc, mag = x[src].double() @ W.t() * f, x[src].double().abs() @ W.abs().t() * f.abs()
+    return acc, (2.0 ** -12 + 2 * W.shape[1] * U) * mag + 4 * U * acc.abs()
+
+
+def check_codes(q, s, h, dh):
+    """Codes and scales of rows whose values are within dh of h."""
+    q, s = q.view(torch.float8_e4m3fn).double(), s.double()
+    want = h.abs().amax(1) / 448
+    assert torch.all((s - want).abs() <= dh.amax(1) / 448 + 2 * U * want)
+    v = h / s[:, None]
+    step = torch.exp2(torch.floor(torch.log2(torch.maximum(v.abs(), q.abs()).clamp_min(2.0 ** -6))) - 3)
+    assert torch.all((q - v).abs() <= step / 2 + dh / s[:, None] + 2 * U * v.abs())
+
+
+def check_h(q, s, x, xs, gate, up, order, offsets, top):
+    """The quantised middle of the MLP against 64 bits.  |silu'| < 1.1 and |silu(g)| <= |g|; exp(-g) is off by
+    2 |g| u for its argument, and exp, division and products add fewer than 16 roundings."""
+    for e in range(gate[1].shape[0]):
+        a, b = int(offsets[e]), int(offsets[e + 1])
+        if a == b:
+            continue
+        src = order[a:b].long() // top
+        g, dg = glu_bounds(x, xs, gate[1][e], gate[2][e], src)
+        u, du = glu_bounds(x, xs, up[1][e], up[2][e], src)
+        silu = g / (1 + torch.exp(-g))
+        h = u * silu
+        check_codes(q[a:b], s[a:b], h, du * silu.abs() + 1.1 * dg * (u.abs() + du) + (2 * g.abs() + 16) * U * h.abs())
+
+
+def kernels(capfd):
+    return [name for name, _, _ in launches(capfd)]
+
+
+@pytest.mark.parametrize("T,top,E,N,K,db,kernel", [
+    (3, 2, 5, 130, 5120, 96, "rows"), (20, 2, 2, 96, 4128, 32, "rows"), (40, 2, 5, 130, 512, 96, "stream"),
+    (90, 2, 4, 160, 320, 160, "stream"), (150, 3, 6, 257, 544, 128, "128x128"), (1040, 1, 8, 1101, 288, 624, "256x256"),
+    (700, 2, 9, 1100, 352, 0, "256x256"), (2600, 1, 10, 700, 256, 700, "256x256"), (300, 2, 3, 3201, 608, 2400, "256x256")])
+def test_pair_against_the_formula(S, capfd, T, top, E, N, K, db, kernel):
+    """G, U and H's codes of a gate / up pair, each against 64 bits, in every kernel that computes two weights."""
+    say(f"[pair] T={T} top={top} E={E} {N}x{K} db={db} {kernel}")
+    g = torch.Generator().manual_seed(T + N + 5)
+    gate, up = weights(S, g, E, N, K, 0, db, False), weights(S, g, E, N, K, 0, db, False)
+    x, xs = tokens(g, T, K, False)
+    xs = xs / K ** 0.5
+    X, XS, sc = x.view(torch.uint8).cuda(), xs.cuda(), [gate[2].cuda(), up[2].cuda()]
+    groups = S.group_rows(choices(g, "even", T, top, E).reshape(-1).cuda(), E)
+    order, offsets = groups.order.cpu(), groups.offsets.cpu()
+    prev = S.spense_set_log(2)
+    try:
+        capfd.readouterr()
+        both = S.gemm_experts(X, [gate[0], up[0]], groups, sc, XS, top=top, out_f32=True)
+        q, s = S.gemm_experts_glu_fp8(X, gate[0], up[0], groups, *sc, XS, top=top)
+        assert kernels(capfd) == [kernel, kernel + (", gate/up paired" if kernel == "256x256" else "")]
+    finally:
+        S.spense_set_log(prev)
+    for y, w in zip(both, (gate, up)):
+        check(y.cpu(), order, offsets, x, xs, w[1], w[2], top, False, True)
+    check_h(q.cpu(), s.cpu(), x, xs, gate, up, order, offsets, top)
+
+
+@pytest.mark.parametrize("T,top,E,H,I,db,which", [
+    (1, 2, 4, 256, 96, 64, ["stream"] * 2), (7, 3, 5, 512, 160, 128, ["stream"] * 2), (2, 2, 3, 3616, 96, 32, ["rows", "stream"]),
+    (300, 2, 2, 256, 128, 0, ["128x128"] * 2), (1300, 2, 2, 1440, 672, 320, ["256x256, gate/up paired", "256x256"])])
+def test_mlp_steps_against_the_formula(S, capfd, T, top, E, H, I, db, which):
+    """The whole MLP: H's codes against 64 bits, then the output against 64 bits from these codes."""
+    say(f"[mlp] T={T} top={top} E={E} hidden={H} inter={I} db={db}")
+    g = torch.Generator().manual_seed(T + I + 7)
+    gate, up = weights(S, g, E, I, H, 0, db, False), weights(S, g, E, I, H, 0, db, False)
+    down = weights(S, g, E, H, I, 1, db, False)
+    x, xs = tokens(g, T, H, False)
+    xs = xs / H ** 0.5
+    idx, w = choices(g, "even", T, top, E), torch.rand(T, top, generator=g)
+    X, XS, sc = x.view(torch.uint8).cuda(), xs.cuda(), [v[2].cuda() for v in (gate, up, down)]
+    prev = S.spense_set_log(2)
+    try:
+        capfd.readouterr()
+        y = S.mlp_experts(X, XS, idx.cuda(), w.cuda(), gate[0], up[0], down[0], *sc).cpu().double()
+        assert kernels(capfd) == which
+    finally:
+        S.spense_set_log(prev)
+    groups = S.group_rows(idx.reshape(-1).cuda(), E)
+    order, offsets = groups.order.cpu().long(), groups.offsets.cpu()
+    q, s = (v.cpu() for v in S.gemm_experts_glu_fp8(X, gate[0], up[0], groups, *sc[:2], XS, top=top))
+    check_h(q, s, x, xs, gate, up, order, offsets, top)
+    want, mag = torch.zeros(T, H, dtype=torch.float64), torch.zeros(T, H, dtype=torch.float64)
+    for e in range(E):
+        p = slice(int(offsets[e]), int(offsets[e + 1]))
+        h = q[p].view(torch.float8_e4m3fn).double() * s[p].double()[:, None]
+        f = down[2][e].double()[None, :] * w.reshape(-1)[order[p], None].double()
+        want.index_add_(0, order[p] // top, h @ down[1][e].t() * f)
+        mag.index_add_(0, order[p] // top, h.abs() @ down[1][e].abs().t() * f)
+    err = (2.0 ** -12 + 2 * I * U + 8 * U) * mag
+    assert torch.all((y - want).abs() <= err + 2.0 ** -8 * (want.abs() + err))
