@@ -595,3 +595,11 @@ def test_mlp_steps_against_the_formula(S, capfd, T, top, E, H, I, db, which):
         mag.index_add_(0, order[p] // top, h.abs() @ down[1][e].abs().t() * f)
     err = (2.0 ** -12 + 2 * I * U + 8 * U) * mag
     assert torch.all((y - want).abs() <= err + 2.0 ** -8 * (want.abs() + err))
+
+
+@pytest.mark.parametrize("T,top,E,N,K,split,db", [(1500, 2, 1000, 40, 64, 0, 16), (9, 8, 1024, 16, 96, 1, 32), (9000, 2, 1000, 16, 32, 0, 16),
+                                                  (18000, 2, 600, 18, 32, 0, 0), (35000, 2, 600, 16, 32, 1, 0)])
+def test_many_experts(S, T, top, E, N, K, split, db):
+    """Up to sixteen experts a lane in the search for a tile, from tiles of 16 positions to tiles of 256."""
+    test_experts_exact(S, T, top, E, N, K, split, db, "even")
+    test_experts_exact(S, T, top, E, N, K, split, db, "skewed")
