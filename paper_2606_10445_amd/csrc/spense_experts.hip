@@ -7,8 +7,9 @@
 // 32 positions: a wave owns 16 weight rows over all of K and keeps three chunks of 512 columns in
 // registers ahead of the one in its matrix instructions; the tile's activations, gathered row by row,
 // go through LDS a chunk at a time, shared by the workgroup's waves.  64 experts of 1536 x 5120, gate
-// and up, 256 rows: 650 MB of weights in 97 us, 6.7 TB/s.  experts_stream_kernel does the same for a
-// short K, in tiles of up to 64 positions.
+// and up, 256 rows that 56 of them get: 633 MB of weights in 95 us, 6.7 TB/s, where a plain read reaches
+// 7.0.  experts_stream_kernel does the same for a short K, in tiles of up to 64 positions.  Both read whole
+// chunks of 512 columns, padding included: 1.45 times the kept bytes where K = 1408 is 1056 2:4 and 352 dense.
 // Many rows: the 128 x 128 and 256 x 256 kernels over tiles of positions (spense_gemm_mid.hip,
 // spense_gemm_big2.hip).
 #include <cstdio>

@@ -6,9 +6,10 @@
 // order).  Inside a wave a lane finds the lanes with its key by ballots over the key's bits; its
 // rank is the number of lower ones.  The order is the index order, whatever the timing.
 //
-// Latency-bound at decode sizes (n = 64: 3.7 us); n = 16384 takes 8 us (one workgroup walking all
-// entries with ballots 22, its CU's vector instructions the bound), 65536 18, 2^20 0.65 ms: the
-// counting grows with n^2 / 1024, so that is the most a call takes.
+// Latency-bound at decode sizes (n = 64: 3.7 us); n = 16384 takes 8 us in a row of such launches, 11
+// behind a copy of 1 GiB, which leaves idx in no cache, 13 in a pass behind a long product (one workgroup
+// walking all entries with ballots 22, its CU's vector instructions the bound), 65536 18, 2^20 0.65 ms:
+// the counting grows with n^2 / 1024, so that is the most a call takes.
 #include <hip/hip_runtime.h>
 
 #include "spense.h"
