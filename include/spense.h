@@ -542,7 +542,8 @@ int spense_obs_prune_24(float* W, int64_t ldw, int64_t N, int64_t K, const float
  * Asynchronous, allocates nothing.
  * SPENSE_ERR_ARG for a NULL x, no output, q without scales, a gate or post_weight without y,
  * M below 0 or too large, K below 1 or above 2^31-1, residual in the place of y or normed, normed in the
- * place of x, an output in its input's place with another leading dimension (M > 1), ld below K, unknown types, a negative or non-finite eps;
+ * place of x, an output in its input's place with another leading dimension (M > 1), ld below K,
+ * unknown types, a negative or non-finite eps;
  * SPENSE_ERR_ALIGN for an operand not aligned to its elements.
  */
 typedef struct spense_block_norm_t {
@@ -711,7 +712,8 @@ int spense_abi_version(void);
  * >= 1 every call that makes a new plan for a single weight (the planner's choice for one
  * dtype, M and weight geometry; later calls with the same key reuse it) writes one line to
  * stderr naming the kernel and its shape; with level >= 2 every grouped and paired call
- * does too, those over rows grouped by expert and spense_add_adapters among them.  The level starts at the value of the environment variable SPENSE_LOG when
+ * does too, those over rows grouped by expert and spense_add_adapters among them.  The
+ * level starts at the value of the environment variable SPENSE_LOG when
  * the library is loaded (0 when unset or not a number); it is read there only.  The log
  * never changes a plan or a result.  Returns the previous level; thread-safe.
  */
